@@ -435,6 +435,137 @@ moeq_status moeq_plan_bits(const moeq_plan_params* p, int32_t n, const int64_t* 
 #define MOEQ_STAGE_EVENTS 5
 moeq_status moeq_set_stage_events(moeq_layer* layer, void* const* events, int32_t count);
 
+/* ---- Paged key/value cache and attention ------------------------------------
+ * The other half of the transformer block around the layer, for serving: a
+ * cache of keys and values in pages, the step's bookkeeping, and the attention
+ * that fills and reads it.  No handle: every buffer is the caller's.  Work is
+ * enqueued on `stream`; nothing is allocated or synchronized, and every call
+ * may be captured in a HIP graph.  Results are deterministic.
+ *
+ * A cache holds n_pages pages of page_size places, for every kv head one key of
+ * head_dim and one value of value_dim values in each place.  Place p of page b
+ * is slot b * page_size + p.  A request's block table lists its pages: the
+ * token at position s lies in page table[s / page_size], place s % page_size. */
+enum { MOEQ_BF16 = 0, MOEQ_F16 = 1 };
+
+/* Head layout and mask of an attention.
+ *   n_heads, n_kv_heads  query heads share kv heads in runs of n_heads /
+ *               n_kv_heads (a whole number, at most 256)
+ *   head_dim, value_dim  (64, 64), (128, 128) or (192, 128) (else UNSUPPORTED)
+ *   dtype       MOEQ_BF16 or MOEQ_F16: queries, keys, values and the output
+ *   causal      1: a token sees the keys up to its own position; 0: all
+ *   window      0: no limit; w > 0 (causal only): the last w of those keys
+ *   scale       factor of the scores, finite and positive
+ * A row that sees no key has output 0 and lse -infinity.  Scores, softmax
+ * statistics and sums are float32; the weights are rounded once to dtype
+ * before they multiply the values, the output once. */
+typedef struct {
+  int32_t n_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t value_dim;
+  int32_t dtype;
+  int32_t causal;
+  int32_t window;
+  float scale;
+} moeq_attn;
+
+/* DEVICE rows of heads: element (t, h, i) at p[t * token_stride + h *
+ * head_stride + i].  p on 16 bytes, strides in elements, non-negative multiples
+ * of 8. */
+typedef struct {
+  void* p;
+  int64_t token_stride;
+  int64_t head_stride;
+} moeq_rows;
+
+/* A cache: key (page, place, head, i) at k[page * k_page_stride + place *
+ * k_slot_stride + head * k_head_stride + i], values likewise.
+ *   k, v        DEVICE, on 16 bytes; strides in elements, non-negative
+ *               multiples of 8, the slot strides below 2^26
+ *   page_size   a power of two, 16 .. 4096
+ *   n_pages     >= 1; n_pages * page_size < 2^31 */
+typedef struct {
+  void* k;
+  void* v;
+  int32_t n_pages;
+  int32_t page_size;
+  int64_t k_page_stride, k_slot_stride, k_head_stride;
+  int64_t v_page_stride, v_slot_stride, v_head_stride;
+} moeq_kv_cache;
+
+/* One step's tables.  Request r holds ctx_lens[r] tokens in the cache and adds
+ * new_lens[r]: > 0 tokens, 0 none, < 0 it is done and gives its pages back.
+ * Pages come, in the requests' order, from the head of a queue of free pages
+ * (a ring of n_pages entries) and go back to its tail.  A request whose pages
+ * do not fit max_blocks, or which needs pages and the pages needed up to and
+ * with it exceed those free at the step's start, is refused: it takes none, its
+ * slots are -1 and its kv_len 0; the others are served.
+ *   ctx_lens, new_lens  DEVICE int32 [n_requests]
+ *   block_table  DEVICE int32 [n_requests x max_blocks], rows table_stride
+ *                apart; the entries of pages taken are written
+ *   free_pages   DEVICE int32 [n_pages], the ring; pages given back are written
+ *   pool_in      DEVICE int32 [3]: head (0 .. n_pages - 1), pages free, ignored
+ *   pool_out     DEVICE int32 [3] (written; may be pool_in): head, pages free,
+ *                requests refused
+ *   n_tokens     the sum of the positive new_lens; tokens beyond it are dropped
+ *   cu_q         DEVICE int32 [n_requests + 1] (written): first token of each
+ *                request, then the total
+ *   kv_lens      DEVICE int32 [n_requests] (written): tokens to attend to
+ *   slots, positions  DEVICE int32 [n_tokens] (written; slots -1 beyond cu_q's total)
+ * Page ids outside [0, n_pages) give slots of -1.
+ * Errors: INVALID_ARG, DEVICE. */
+moeq_status moeq_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int32_t n_requests, int32_t* block_table,
+                         int64_t table_stride, int32_t max_blocks, int32_t* free_pages, int32_t n_pages,
+                         const int32_t* pool_in, int32_t* pool_out, int32_t page_size, int32_t n_tokens, int32_t* cu_q,
+                         int32_t* kv_lens, int32_t* slots, int32_t* positions, void* stream);
+
+/* Stores token t's keys and values in slot slots[t]; slots outside the cache
+ * (-1) are skipped.  Distinct tokens' slots must differ.
+ *   head, n_kv_heads, head_dim, value_dim, dtype of `a` are used; any dims that
+ *   are multiples of 8 up to 1024 serve here
+ *   k, v    DEVICE [n_tokens x n_kv_heads x head_dim / value_dim]
+ *   slots   DEVICE int32 [n_tokens]
+ * Errors: INVALID_ARG, DEVICE. */
+moeq_status moeq_kv_append(const moeq_attn* a, const moeq_kv_cache* cache, const moeq_rows* k, const moeq_rows* v,
+                           const int32_t* slots, int32_t n_tokens, void* stream);
+
+/* Attention over whole prompts packed one after another: tokens cu[s] ..
+ * cu[s + 1] - 1 are sequence s and see each other only.
+ *   q, k, v   DEVICE rows [n_tokens x heads x dims]
+ *   cu        DEVICE int32 [n_seqs + 1], ascending, within 0 .. n_tokens
+ *   out       DEVICE rows [n_tokens x n_heads x value_dim] (written)
+ *   lse       DEVICE float [n_tokens x n_heads] (written): natural logarithm of
+ *             each row's sum of exponentials; or NULL
+ * Tokens of no sequence are not written.
+ * Errors: INVALID_ARG, UNSUPPORTED, DEVICE. */
+moeq_status moeq_attn_prompt(const moeq_attn* a, const moeq_rows* q, const moeq_rows* k, const moeq_rows* v,
+                             const int32_t* cu, int32_t n_seqs, int32_t n_tokens, const moeq_rows* out, float* lse,
+                             void* stream);
+
+/* Attention of each request's new tokens over the cache (which holds their own
+ * keys and values already): token j of request r's n = cu_q[r + 1] - cu_q[r] is
+ * at position kv_lens[r] - n + j; rows before position 0 see nothing.
+ *   cu_q         DEVICE int32 [n_requests + 1], ascending, within 0 .. n_tokens
+ *   kv_lens      DEVICE int32 [n_requests]
+ *   block_table  DEVICE int32 [n_requests x max_blocks], rows table_stride
+ *                apart; the entries of the pages below kv_lens[r] must be pages
+ *                of the cache (other values are not followed outside it, but
+ *                what they contribute is unspecified)
+ *   n_tokens     rows of q and out
+ *   max_new      at least the most new tokens of a request (a larger request
+ *                may be left out)
+ *   workspace    DEVICE, on 256 bytes, at least moeq_attn_paged_workspace's
+ *                bytes; need not be cleared, holds nothing between calls
+ *   lse          as for moeq_attn_prompt, or NULL
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (workspace), DEVICE. */
+moeq_status moeq_attn_paged(const moeq_attn* a, const moeq_rows* q, const moeq_kv_cache* cache, const int32_t* cu_q,
+                            const int32_t* kv_lens, const int32_t* block_table, int64_t table_stride,
+                            int32_t max_blocks, int32_t n_requests, int32_t n_tokens, int32_t max_new,
+                            const moeq_rows* out, float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+/* Bytes of its workspace, for any lengths (host only). */
+moeq_status moeq_attn_paged_workspace(const moeq_attn* a, int32_t max_new, uint64_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,738 @@
+// Attention over packed prompts and over a paged cache.
+//
+// Row r of sequence s and kv head h is query token r / g, head h g + r % g (g
+// query heads share a kv head): the rows that read the same keys form tiles.
+#include "attn_core.h"
+#include "attention.h"
+
+namespace moeq {
+
+namespace {
+
+// read-only during a kernel: scalar loads
+typedef const __attribute__((address_space(4))) int32_t CInt;
+__device__ __forceinline__ int cload(const int32_t* p, int64_t i) { return ((CInt*)p)[i]; }
+
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
+
+// s_barrier after this wave's loads into LDS have landed and its LDS reads have returned
+__device__ __forceinline__ void stage_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+}
+
+// One sequence's part of a launch: its query tokens and its keys.  Bounds hold
+// for any contents of cu and kv_lens.
+struct Seq {
+  int start, n, kv;  // first query token (row of q), query tokens, keys
+};
+__device__ __forceinline__ Seq prompt_seq(const AttnArgs& a, int s) {
+  const int b = clampi(cload(a.cu, s), 0, a.T), e = clampi(cload(a.cu, s + 1), b, a.T);
+  return Seq{b, e - b, e - b};
+}
+__device__ __forceinline__ Seq paged_seq(const AttnArgs& a, int r) {
+  const int b = clampi(a.cu[r], 0, a.T), e = clampi(a.cu[r + 1], b, a.T);
+  return Seq{b, e - b, clampi(a.kv_lens[r], 0, a.max_kv)};
+}
+
+// Keys that the query token at index j of a sequence sees: [lo, hi).
+struct Span {
+  int lo, hi;
+};
+__device__ __forceinline__ Span visible(const AttnArgs& a, const Seq& s, int j) {
+  if (!a.causal) return Span{0, s.kv};
+  const int p = s.kv - s.n + j;  // its position
+  const int hi = max(p + 1, 0);
+  return Span{a.window ? max(hi - a.window, 0) : 0, hi};
+}
+
+// Where a sequence's keys and values lie, and the loads of 16 of them into LDS.
+template <int D, int DV, bool PAGED>
+struct Keys {
+  const AttnArgs& a;
+  const char *k, *v;
+  const int32_t* table;
+  int kv;
+  GranuleOffsets<D / 8, true> ko;
+  GranuleOffsets<DV / 8, false> vo;
+  __device__ __forceinline__ explicit Keys(const AttnArgs& args) : a(args) {
+    ko.set(a.k_row, kGranule - 1);
+    vo.set(a.v_row, kGranule - 1);
+  }
+  __device__ __forceinline__ void seq(const Seq& s, int r, int head) {
+    k = a.k + (int64_t)head * a.k_head;
+    v = a.v + (int64_t)head * a.v_head;
+    kv = s.kv;
+    if constexpr (PAGED) {
+      table = a.table + (int64_t)r * a.table_stride;
+    } else {
+      k += (int64_t)s.start * a.k_row;
+      v += (int64_t)s.start * a.v_row;
+    }
+  }
+  // the first of the keys' granule of 16 that is loaded for keys key .. key + 15:
+  // the last one that holds a key, if theirs does not
+  __device__ __forceinline__ int granule(int key) const { return min(key, (kv - 1) & ~(kGranule - 1)); }
+  __device__ __forceinline__ int page(int g) const {
+    if constexpr (!PAGED) return 0;
+    const int b = cload(table, g >> a.page_shift);
+    return (uint32_t)b < (uint32_t)a.n_pages ? b : 0;
+  }
+  __device__ __forceinline__ const char* value_row(int key) const {
+    if constexpr (!PAGED) return v + (int64_t)key * a.v_row;
+    const int g = key & ~(kGranule - 1);
+    return v + page(g) * a.v_page + (int64_t)(key & ((1 << a.page_shift) - 1)) * a.v_row;
+  }
+  __device__ __forceinline__ void load(int g, int page, uint32_t k_dst, uint32_t v_dst) const {
+    const char *kp, *vp;
+    if constexpr (PAGED) {
+      const int at = g & ((1 << a.page_shift) - 1);
+      kp = k + page * a.k_page + (int64_t)at * a.k_row;
+      vp = v + page * a.v_page + (int64_t)at * a.v_row;
+    } else {
+      kp = k + (int64_t)g * a.k_row;
+      vp = v + (int64_t)g * a.v_row;
+    }
+    if (g + kGranule <= kv) {
+      ko.load(kp, k_dst);
+      vo.load(vp, v_dst);
+    } else {  // rows past the last key repeat it (they are masked; what lies there may be anything)
+      GranuleOffsets<D / 8, true> kt;
+      GranuleOffsets<DV / 8, false> vt;
+      kt.set(a.k_row, kv - 1 - g);
+      vt.set(a.v_row, kv - 1 - g);
+      kt.load(kp, k_dst);
+      vt.load(vp, v_dst);
+    }
+  }
+};
+
+// The lane's row of a tile of rows that starts at row0
+struct Row {
+  int token, head;  // within the sequence; within the kv head's query heads
+  bool valid;
+  Span see;
+};
+__device__ __forceinline__ Row row_of(const AttnArgs& a, const Seq& s, int row) {
+  Row r;
+  r.valid = row < s.n * a.g;
+  r.token = row / a.g;
+  r.head = row - r.token * a.g;
+  r.see = r.valid ? visible(a, s, r.token) : Span{0, 0x7FFFFFFF};
+  return r;
+}
+
+template <typename T, int DV, int DB>
+__device__ __forceinline__ void store_out(const AttnArgs& a, const f32x16 (&o)[DB], float m, float l, const Seq& s,
+                                          const Row& r, int kvh) {
+  const int h = (threadIdx.x >> 5) & 1;
+  const int head = kvh * a.g + r.head;
+  const float inv = l > 0.0f || !(l == l) ? 1.0f / l : 0.0f;
+  char* row = a.out + (int64_t)(s.start + r.token) * a.o_row + (int64_t)head * a.o_head;
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      // registers 8 t .. + 3 hold columns 16 t + 4 h .. + 3, the next four
+      // those 8 further: after the swap a lane holds 8 columns in a row
+      uint32_t x[2], y[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[i] = T::pack(o[b][8 * t + 2 * i] * inv, o[b][8 * t + 2 * i + 1] * inv);
+        y[i] = T::pack(o[b][8 * t + 4 + 2 * i] * inv, o[b][8 * t + 4 + 2 * i + 1] * inv);
+      }
+      const auto u = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
+      const auto w = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+      if (r.valid) *(u32x4*)(row + (32 * b + 16 * t + 8 * h) * 2) = u32x4{u[0], w[0], u[1], w[1]};
+    }
+  if (a.lse && r.valid && h == 0)
+    a.lse[(int64_t)(s.start + r.token) * a.HQ + head] = m == kLowest ? -INFINITY : m * a.scale + __logf(l);
+}
+
+// ---- tiles of 32 rows a wave ----
+// The workgroup's waves share key tiles of 64 (NW waves: each loads 64 / NW /
+// 16 granules) in two stages of LDS; each wave keeps 32 rows.
+constexpr int kTileKeys = 64;
+
+template <typename T, int D, int DV, int NW, bool PAGED>
+struct TileKernel {
+  static constexpr int BM = 32 * NW;
+  static constexpr uint32_t kK = kTileKeys * D * 2, kV = kTileKeys * DV * 2, kStage = kK + kV;
+  static constexpr size_t lds = 2 * kStage;
+  typedef RowBlock<T, D, DV> RB;
+
+  // The tile's rows' keys [lo, hi) -> rb.  all: the keys that every row sees.
+  // Tiles within `all` take no mask; those before and after have code of their own,
+  // so that the main loop holds nothing else.
+  static __device__ __forceinline__ void run(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
+                                             const Keys<D, DV, PAGED>& keys, const Row& r, int lo, int hi, Span all) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nt = (hi - lo + kTileKeys - 1) / kTileKeys;
+    const int a0 = min(nt, (max(all.lo - lo, 0) + kTileKeys - 1) / kTileKeys);
+    const int a1 = clampi((min(all.hi, hi) - lo) / kTileKeys, a0, nt);
+    auto load = [&](int t) {
+      const uint32_t st = base + (t & 1) * kStage;
+      const int g = keys.granule(lo + t * kTileKeys + wave * kGranule);
+      keys.load(g, keys.page(g), st + wave * (kGranule * D * 2), st + kK + wave * (kGranule * DV * 2));
+    };
+    static_assert(NW * kGranule == kTileKeys, "one granule a wave");
+    Span odd{0x7FFFFFFF, 0};  // of the blocks whose values add_nonfinite adds
+    auto tile = [&](int t, auto masked) {
+      stage_barrier();
+      if (t + 1 < nt) load(t + 1);
+      const int key = lo + t * kTileKeys, top = min(r.see.hi, keys.kv);
+      if constexpr (decltype(masked)::value)
+        if (!__any(r.valid && top > key && r.see.lo < key + kTileKeys)) return;
+      const uint32_t kt = base + (t & 1) * kStage, vt = kt + kK;
+      f32x16 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) s[b] = rb.scores(ad, kt + b * 32 * D * 2);
+      if constexpr (decltype(masked)::value)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) RB::mask(s[b], key + 32 * b, r.see.lo, top);
+      uint32_t p[2][8];
+      rb.template softmax<2>(s, a.c, p);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint32_t v = vt + b * 32 * DV * 2;
+        const bool finite = decltype(masked)::value && RB::any_nonfinite(v);
+        if (finite) {
+          odd.lo = min(odd.lo, key + 32 * b);
+          odd.hi = key + 32 * b + 32;
+        }
+        rb.template values<decltype(masked)::value>(ad, v, p[b], finite);
+      }
+    };
+    if (nt > 0) load(0);
+    int t = 0;
+    for (; t < a0; ++t) tile(t, std::true_type());
+    for (; t < a1; ++t) tile(t, std::false_type());
+    for (; t < nt; ++t) tile(t, std::true_type());
+    if (odd.lo < odd.hi)
+      rb.add_nonfinite(odd.lo, min(odd.hi, hi), r.see.lo, r.see.hi, [&](int key) { return keys.value_row(key); });
+    stage_barrier();
+  }
+};
+
+// Grid: (kv heads) x (tile slots).  Sequence s has the slots from
+// floor(cu[s] g / BM) + s on: as many as its tiles, or one more, whatever the
+// lengths, so the grid follows from the totals alone.
+template <typename T, int D, int DV, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
+  typedef TileKernel<T, D, DV, NW, false> TK;
+  extern __shared__ char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Workgroup b runs on XCD b % 8.  With a multiple of 8 kv heads an XCD takes
+  // whole heads, one after the other, so that its L2 holds their keys; late
+  // tiles, which see the most keys, come first.
+  const int b = blockIdx.x;
+  int kvh, slot;
+  if (a.HK % 8 == 0) {
+    const int j = b >> 3;
+    kvh = (b & 7) + 8 * (j / a.n_slots);
+    slot = a.n_slots - 1 - j % a.n_slots;
+  } else {
+    kvh = b % a.HK;
+    slot = a.n_slots - 1 - b / a.HK;
+  }
+  auto first_slot = [&](int s) { return (int)((int64_t)clampi(a.cu[s], 0, a.T) * a.g / TK::BM) + s; };
+  int seq = 0;
+  for (int n = a.n_seqs; n > 1;) {  // the last sequence whose first slot is not beyond `slot`, 64 probes at a time
+    const int step = (n + 63) / 64, i = lane * step;
+    const int c = __popcll(__ballot(i < n && first_slot(seq + i) <= slot));
+    const int skip = (max(c, 1) - 1) * step;
+    seq += skip;
+    n = min(step, n - skip);
+  }
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  const Seq s = prompt_seq(a, seq);
+  const int row0 = (slot - __builtin_amdgcn_readfirstlane(first_slot(seq))) * TK::BM;
+  if (row0 < 0 || row0 >= s.n * a.g) return;
+  const Row r = row_of(a, s, row0 + wave * 32 + (lane & 31));
+  const int last = min(row0 + TK::BM, s.n * a.g) - 1;
+  const Span v0 = visible(a, s, row0 / a.g), v1 = visible(a, s, last / a.g);
+  const int lo = v0.lo & ~(kGranule - 1), hi = min(v1.hi, s.kv);
+
+  typename TK::RB rb;
+  typename TK::RB::Addr ad;
+  ad.set();
+  rb.clear();
+  rb.load_q(r.valid ? a.q + (int64_t)(s.start + r.token) * a.q_row + (int64_t)(kvh * a.g + r.head) * a.q_head : nullptr);
+  Keys<D, DV, false> keys(a);
+  keys.seq(s, seq, kvh);
+  TK::run(a, lds_addr(smem), rb, ad, keys, r, lo, hi, Span{v1.lo, min(v0.hi, s.kv)});
+  store_out<T, DV>(a, rb.o, rb.m, sum_halves(rb.l), s, r, kvh);
+}
+
+// ---- the paged cache ----
+// The work of a launch is the key tiles of all (kv head, request, row tile)
+// segments one after another, cut into equal runs for the workgroups whatever
+// the lengths: a segment that one workgroup holds whole is written directly,
+// pieces of one leave partial sums that paged_join_kernel adds up.  A workgroup
+// leaves at most two: the piece it starts with (slot 2 w) and the one it ends
+// with (slot 2 w + 1).
+template <int BM, int BN, bool FEW>
+struct Work {
+  static constexpr bool kFew = FEW;
+  // requests of at most 32 rows go to the few-rows kernel, the others to tiles
+  static __device__ __forceinline__ int row_tiles(const AttnArgs& a, const Seq& s) {
+    const int rows = s.n * a.g;
+    if constexpr (FEW) return rows > 0 && rows <= kFewRows ? 1 : 0;
+    return rows > kFewRows ? (rows + BM - 1) / BM : 0;
+  }
+  static __device__ __forceinline__ Span span(const AttnArgs& a, const Seq& s, int qt) {
+    const int rows = s.n * a.g, row0 = qt * BM, last = min(row0 + BM, rows) - 1;
+    const int hi = min(visible(a, s, last / a.g).hi, s.kv);
+    return Span{min(visible(a, s, row0 / a.g).lo, hi) & ~(kGranule - 1), hi};
+  }
+  // at least 1: rows that see nothing are written too
+  static __device__ __forceinline__ int key_tiles(const Span& p) { return max(1, (p.hi - p.lo + BN - 1) / BN); }
+  static __device__ __forceinline__ long long units(const AttnArgs& a, const Seq& s) {
+    long long u = 0;
+    for (int qt = 0, n = row_tiles(a, s); qt < n; ++qt) u += key_tiles(span(a, s, qt));
+    return u;
+  }
+};
+
+__device__ __forceinline__ long long uniform64(long long v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (long long)(((uint64_t)hi << 32) | lo);
+}
+
+struct Place {
+  long long total;   // units of one kv head
+  long long before;  // units of the requests before r
+  int r;
+};
+// The request that unit `want(total)` of a kv head falls in; every thread of the NT gets it.
+template <typename W, int NT, typename F>
+__device__ Place find_place(const AttnArgs& a, F want) {
+  __shared__ long long wsum[NT / 64];
+  __shared__ long long found_before;
+  __shared__ int found_r;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.n_seqs + NT - 1) / NT, r0 = min(tid * per, a.n_seqs), r1 = min(r0 + per, a.n_seqs);
+  long long own = 0;
+  for (int r = r0; r < r1; ++r) own += W::units(a, paged_seq(a, r));
+  long long incl = own;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long o = __shfl_up(incl, d, 64);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 63) wsum[wave] = incl;
+  __syncthreads();
+  long long total = 0, base = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    if (w < wave) base += wsum[w];
+    total += wsum[w];
+  }
+  total = uniform64(total);
+  long long at = base + incl - own;
+  const long long p = want(total);
+  if (p >= at && p < at + own) {
+    for (int r = r0; r < r1; ++r) {
+      const long long u = W::units(a, paged_seq(a, r));
+      if (p < at + u) {
+        found_r = r;
+        found_before = at;
+        break;
+      }
+      at += u;
+    }
+  }
+  __syncthreads();
+  Place pl{total, 0, 0};
+  if (total > 0) {
+    pl.before = uniform64(found_before);
+    pl.r = __builtin_amdgcn_readfirstlane(found_r);
+  }
+  return pl;
+}
+
+// first unit of run w of G over n >= G units
+__device__ __forceinline__ long long run_start(long long n, int w, int G) { return n * w / G; }
+
+__device__ __forceinline__ Seq uniform(const Seq& s) {
+  return Seq{__builtin_amdgcn_readfirstlane(s.start), __builtin_amdgcn_readfirstlane(s.n),
+             __builtin_amdgcn_readfirstlane(s.kv)};
+}
+
+// Calls segment(kvh, r, seq, qt, span, first key tile, key tiles, whole, slot)
+// for every piece of this workgroup's run.
+template <typename W, int NT, typename F>
+__device__ __forceinline__ void each_piece(const AttnArgs& a, PagedJoin* join, F segment) {
+  const int lane = threadIdx.x & 63;
+  int w = blockIdx.x, G = a.n_wg;  // this workgroup's run and the runs that there are
+  long long pos = 0, end = 0, N = 0;
+  const Place pl = find_place<W, NT>(a, [&](long long total) {
+    N = total * a.HK;
+    if (N < G)
+      G = (int)N;  // one unit a run
+    else if constexpr (!W::kFew)
+      // Workgroup b runs on XCD b % 8: an XCD's runs are neighbours, whose rows
+      // share keys and values (n_wg is a multiple of 8)
+      w = (w & 7) * (G >> 3) + (w >> 3);
+    if (w < G) {
+      pos = run_start(N, w, G);
+      end = run_start(N, w + 1, G);
+    }
+    return total ? pos % total : 0;
+  });
+  PagedJoin rec{0, 0, 0, 0, 0};
+  if (pos < end) {
+    int kvh = (int)(pos / pl.total), r = pl.r, qt = 0;
+    long long off = pos % pl.total - pl.before;
+    Seq s = uniform(paged_seq(a, r));
+    while (pos < end) {
+      const Span sp = W::span(a, s, qt);
+      const int n = W::key_tiles(sp);
+      if (off < n) {
+        const int t0 = (int)off, m = (int)min((long long)(n - t0), end - pos);
+        const bool whole = m == n;
+        segment(kvh, r, s, qt, sp, t0, m, whole, 2 * w + (t0 == 0 ? 1 : 0));
+        if (t0 == 0 && !whole) {
+          // the runs that start before the segment's end: those before ceil(end G / N)
+          const int parts = (int)(((pos + n) * G + N - 1) / N) - w;
+          rec = PagedJoin{parts, s.start, s.n, qt, kvh};
+        }
+        pos += m;
+        off = n;
+      }
+      off -= n;
+      if (++qt >= W::row_tiles(a, s)) {
+        qt = 0;
+        // the next request with work
+        for (++r;; r += 64) {
+          if (r >= a.n_seqs) {
+            ++kvh;
+            r = 0;
+            if (kvh >= a.HK) break;
+          }
+          const uint64_t some = __ballot(r + lane < a.n_seqs && W::row_tiles(a, paged_seq(a, min(r + lane, a.n_seqs - 1))) > 0);
+          if (some) {
+            r += __builtin_ctzll(some);
+            break;
+          }
+        }
+        if (kvh >= a.HK) break;
+        s = uniform(paged_seq(a, r));
+      }
+    }
+  }
+  if (threadIdx.x == 0) join[w] = rec;  // (w < n_wg whatever G is)
+}
+
+__device__ __forceinline__ int64_t part_row(int slot, int row, int BM) { return (int64_t)slot * BM + row; }
+
+// requests of more than 32 rows
+template <typename T, int D, int DV, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
+  typedef TileKernel<T, D, DV, NW, true> TK;
+  typedef Work<TK::BM, kTileKeys, false> W;
+  extern __shared__ char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  typename TK::RB rb;
+  typename TK::RB::Addr ad;
+  ad.set();
+  Keys<D, DV, true> keys(a);
+  each_piece<W, 64 * NW>(a, a.tile_join, [&](int kvh, int r, const Seq& s, int qt, const Span& sp, int t0, int n, bool whole, int slot) {
+    const int in = wave * 32 + (lane & 31);
+    const Row row = row_of(a, s, qt * TK::BM + in);
+    rb.clear();
+    rb.load_q(row.valid ? a.q + (int64_t)(s.start + row.token) * a.q_row + (int64_t)(kvh * a.g + row.head) * a.q_head
+                        : nullptr);
+    keys.seq(s, r, kvh);
+    const int lo = sp.lo + t0 * kTileKeys;
+    const int row0 = qt * TK::BM, last = min(row0 + TK::BM, s.n * a.g) - 1;
+    TK::run(a, lds_addr(smem), rb, ad, keys, row, lo, min(sp.hi, lo + n * kTileKeys),
+            Span{visible(a, s, last / a.g).lo, min(visible(a, s, row0 / a.g).hi, s.kv)});
+    const float l = sum_halves(rb.l);
+    if (whole) {
+      store_out<T, DV>(a, rb.o, rb.m, l, s, row, kvh);
+    } else if (row.valid) {
+      const int64_t at = part_row(slot, in, TK::BM);
+      const int h = lane >> 5;
+#pragma unroll
+      for (int b = 0; b < TK::RB::DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *(f32x4*)(a.tile_part + at * DV + 32 * b + 2 * i + 4 * h) =
+              f32x4{rb.o[b][i], rb.o[b][i + 1], rb.o[b][i + 2], rb.o[b][i + 3]};
+      if (h == 0) {
+        a.tile_ml[2 * at] = rb.m;
+        a.tile_ml[2 * at + 1] = l;
+      }
+    }
+  });
+}
+
+// Requests of at most 32 rows (single tokens above all): the waves take 32 keys
+// each of a tile of 32 NW, through two LDS stages of their own, and join their
+// sums at the end of a piece.
+template <typename T, int D, int DV, int NW>
+struct FewKernel {
+  static constexpr int BN = 32 * NW;
+  static constexpr uint32_t kK = 32 * D * 2, kV = 32 * DV * 2, kStage = kK + kV, kWave = 2 * kStage;
+  static constexpr int kLoads = 2 * (D / 32 + DV / 32);  // of a stage
+  static constexpr int kPitch = DV + 4;                  // floats of a row in the join
+  static constexpr size_t lds = NW * kWave;
+  static_assert(kFewRows * kPitch * 4 <= kWave, "a wave's sums fit its stages");
+};
+
+template <typename T, int D, int DV, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
+  typedef FewKernel<T, D, DV, NW> FK;
+  typedef RowBlock<T, D, DV> RB;
+  typedef Work<kFewRows, FK::BN, true> W;
+  extern __shared__ char smem[];
+  __shared__ float ml[NW][kFewRows][2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5;
+  const uint32_t mine = lds_addr(smem) + wave * FK::kWave;
+  RB rb;
+  typename RB::Addr ad;
+  ad.set();
+  Keys<D, DV, true> keys(a);
+  each_piece<W, 64 * NW>(a, a.few_join, [&](int kvh, int r, const Seq& s, int, const Span& sp, int t0, int n, bool whole, int slot) {
+    const Row row = row_of(a, s, lane & 31);
+    rb.clear();
+    rb.load_q(row.valid ? a.q + (int64_t)(s.start + row.token) * a.q_row + (int64_t)(kvh * a.g + row.head) * a.q_head
+                        : nullptr);
+    keys.seq(s, r, kvh);
+    const int first = sp.lo + t0 * FK::BN + wave * 32;
+    // this wave's tiles: those with a key below sp.hi
+    const int mine_n = min(n, max(0, (sp.hi - first + FK::BN - 1) / FK::BN));
+    auto load = [&](int t) {
+      const uint32_t st = mine + (t & 1) * FK::kStage;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int g = keys.granule(first + t * FK::BN + i * kGranule);
+        keys.load(g, keys.page(g), st + i * (kGranule * D * 2), st + FK::kK + i * (kGranule * DV * 2));
+      }
+    };
+    Span odd{0x7FFFFFFF, 0};
+    if (mine_n > 0) load(0);
+    if (mine_n > 1) load(1);
+    for (int t = 0; t < mine_n; ++t) {
+      if (t + 1 < mine_n)
+        wait_loads<FK::kLoads>();
+      else
+        wait_loads<0>();
+      const int key = first + t * FK::BN;
+      const uint32_t kt = mine + (t & 1) * FK::kStage;
+      f32x16 sc[1];
+      sc[0] = rb.scores(ad, kt);
+      const int top = min(row.see.hi, s.kv);
+      const bool hides = __any(row.see.lo > key || top < key + 32);
+      if (hides) RB::mask(sc[0], key, row.see.lo, top);
+      uint32_t p[1][8];
+      rb.template softmax<1>(sc, a.c, p);
+      const bool finite = hides && RB::any_nonfinite(kt + FK::kK);
+      if (finite) {
+        odd.lo = min(odd.lo, key);
+        odd.hi = key + 32;
+      }
+      rb.template values<true>(ad, kt + FK::kK, p[0], finite);
+      wait_lds();
+      if (t + 2 < mine_n) load(t + 2);
+    }
+    if (odd.lo < odd.hi) {
+      // this wave's blocks only: 32 keys every BN
+      for (int key = odd.lo; key < min(odd.hi, s.kv); key += FK::BN)
+        rb.add_nonfinite(key, min(key + 32, s.kv), row.see.lo, row.see.hi, [&](int k) { return keys.value_row(k); });
+    }
+    // join the waves
+    const float l = sum_halves(rb.l);
+    if (h == 0) {
+      ml[wave][lane][0] = rb.m;
+      ml[wave][lane][1] = l;
+    }
+    __syncthreads();
+    float M = kLowest, L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w][lane & 31][0]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float mw = ml[w][lane & 31][0];
+      L += mw == kLowest ? 0.0f : ml[w][lane & 31][1] * exp2_fast((mw - M) * a.c);
+    }
+    const float f = rb.m == kLowest ? 0.0f : exp2_fast((rb.m - M) * a.c);
+    float* so = (float*)(smem + wave * FK::kWave) + (lane & 31) * FK::kPitch;
+#pragma unroll
+    for (int b = 0; b < RB::DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4*)(so + 32 * b + 2 * i + 4 * h) =
+            f32x4{rb.o[b][i] * f, rb.o[b][i + 1] * f, rb.o[b][i + 2] * f, rb.o[b][i + 3] * f};
+    // a row's joined statistics, in its last wave's slot once every wave has read it
+    __syncthreads();
+    if (wave == 0 && h == 0) {
+      ml[0][lane][0] = M;
+      ml[0][lane][1] = L;
+    }
+    __syncthreads();
+    const int rows = s.n * a.g;
+    for (int i = tid; i < rows * (DV / 8); i += 64 * NW) {
+      const int rr = i / (DV / 8), col = i % (DV / 8) * 8;
+      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float* p = (const float*)(smem + w * FK::kWave) + rr * FK::kPitch + col;
+        x += *(const f32x4*)p;
+        y += *(const f32x4*)(p + 4);
+      }
+      const float m = ml[0][rr][0], lr = ml[0][rr][1];
+      if (whole) {
+        const float inv = lr > 0.0f || !(lr == lr) ? 1.0f / lr : 0.0f;
+        const int token = rr / a.g, head = kvh * a.g + rr - token * a.g;
+        *(u32x4*)(a.out + (int64_t)(s.start + token) * a.o_row + (int64_t)head * a.o_head + col * 2) =
+            u32x4{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv), T::pack(y[0] * inv, y[1] * inv),
+                  T::pack(y[2] * inv, y[3] * inv)};
+        if (a.lse && col == 0)
+          a.lse[(int64_t)(s.start + token) * a.HQ + head] = m == kLowest ? -INFINITY : m * a.scale + __logf(lr);
+      } else {
+        const int64_t at = part_row(slot, rr, kFewRows);
+        *(f32x4*)(a.few_part + at * DV + col) = x;
+        *(f32x4*)(a.few_part + at * DV + col + 4) = y;
+        if (col == 0) {
+          a.few_ml[2 * at] = m;
+          a.few_ml[2 * at + 1] = lr;
+        }
+      }
+    }
+    __syncthreads();
+  });
+}
+
+// Adds up the pieces of the segments that were cut: workgroup (w, y), wave by
+// row; one wave a row, DV / 64 columns a lane.
+template <typename T, int DV, int BM>
+__global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, const PagedJoin* join, const float* part,
+                                                        const float* ml) {
+  constexpr int NC = DV / 64;
+  const int w = blockIdx.x;
+  const PagedJoin rec = join[w];
+  if (rec.parts == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row0 = rec.row_tile * BM, rows = min(BM, rec.n * a.g - row0);
+  for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
+    auto slot = [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); };
+    float M = kLowest;
+    for (int i = lane; i < rec.parts; i += 64) M = fmaxf(M, ml[2 * part_row(slot(i), row, BM)]);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
+    float L = 0.0f, o[NC] = {};
+    for (int i = 0; i < rec.parts; ++i) {
+      const int64_t at = part_row(slot(i), row, BM);
+      const float mi = ml[2 * at];
+      const float f = mi == kLowest ? 0.0f : exp2_fast((mi - M) * a.c);
+      L += f * ml[2 * at + 1];
+#pragma unroll
+      for (int j = 0; j < NC; ++j) o[j] += f * part[at * DV + lane * NC + j];
+    }
+    const float inv = L > 0.0f || !(L == L) ? 1.0f / L : 0.0f;
+    const int token = (row0 + row) / a.g, head = rec.kvh * a.g + (row0 + row) % a.g;
+    char* out = a.out + (int64_t)(rec.start + token) * a.o_row + (int64_t)head * a.o_head;
+    const uint32_t u = T::pack(o[0] * inv, o[NC - 1] * inv);
+    if constexpr (NC == 2)
+      *(uint32_t*)(out + lane * 4) = u;
+    else
+      *(uint16_t*)(out + lane * 2) = (uint16_t)u;
+    if (a.lse && lane == 0)
+      a.lse[(int64_t)(rec.start + token) * a.HQ + head] = M == kLowest ? -INFINITY : M * a.scale + __logf(L);
+  }
+}
+
+template <typename F>
+hipError_t by_type(int dtype, int D, F f) {
+  if (dtype == MOEQ_BF16) {
+    if (D == 64) return f(Bf16(), std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
+    if (D == 128) return f(Bf16(), std::integral_constant<int, 128>(), std::integral_constant<int, 128>());
+    return f(Bf16(), std::integral_constant<int, 192>(), std::integral_constant<int, 128>());
+  }
+  if (D == 64) return f(F16(), std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
+  if (D == 128) return f(F16(), std::integral_constant<int, 128>(), std::integral_constant<int, 128>());
+  return f(F16(), std::integral_constant<int, 192>(), std::integral_constant<int, 128>());
+}
+
+constexpr int kPromptWaves = 4;
+
+}  // namespace
+
+hipError_t launch_attn_prompt(AttnArgs a, int dtype, int D, hipStream_t s) {
+  return by_type(dtype, D, [&](auto t, auto d, auto dv) -> hipError_t {
+    typedef decltype(t) T;
+    constexpr int NW = kPromptWaves;
+    typedef TileKernel<T, d.value, dv.value, NW, false> TK;
+    static std::atomic<uint64_t> done{0};
+    auto kernel = prompt_kernel<T, d.value, dv.value, NW>;
+    const hipError_t e = raise_lds_limit((const void*)kernel, done, TK::lds);
+    if (e != hipSuccess) return e;
+    const long long slots = (long long)a.T * a.g / TK::BM + a.n_seqs;
+    a.n_slots = (int)slots;
+    kernel<<<(unsigned)(slots * a.HK), 64 * NW, TK::lds, s>>>(a);
+    return hipGetLastError();
+  });
+}
+
+PagedLayout paged_layout(int DV, bool tiles) {
+  PagedLayout l{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = (off + bytes + 255) / 256 * 256;
+    return at;
+  };
+  l.few_join = take(sizeof(PagedJoin) * kFewGroups);
+  l.few_ml = take((size_t)2 * kFewGroups * kFewRows * 8);
+  l.few_part = take((size_t)2 * kFewGroups * kFewRows * DV * 4);
+  if (tiles) {
+    l.tile_join = take(sizeof(PagedJoin) * kTileGroups);
+    l.tile_ml = take((size_t)2 * kTileGroups * 32 * kPromptWaves * 8);
+    l.tile_part = take((size_t)2 * kTileGroups * 32 * kPromptWaves * DV * 4);
+  }
+  l.total = off;
+  return l;
+}
+
+hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipStream_t s) {
+  return by_type(dtype, D, [&](auto t, auto d, auto dv) -> hipError_t {
+    typedef decltype(t) T;
+    constexpr int DV = dv.value;
+    const PagedLayout l = paged_layout(DV, tiles);
+    a.few_join = (PagedJoin*)(ws + l.few_join);
+    a.few_ml = (float*)(ws + l.few_ml);
+    a.few_part = (float*)(ws + l.few_part);
+    a.tile_join = (PagedJoin*)(ws + l.tile_join);
+    a.tile_ml = (float*)(ws + l.tile_ml);
+    a.tile_part = (float*)(ws + l.tile_part);
+    hipError_t e;
+    {
+      constexpr int NW = d.value == 192 ? 3 : 4;  // 160 KB of LDS
+      typedef FewKernel<T, d.value, DV, NW> FK;
+      static std::atomic<uint64_t> done{0};
+      auto kernel = paged_few_kernel<T, d.value, DV, NW>;
+      if ((e = raise_lds_limit((const void*)kernel, done, FK::lds)) != hipSuccess) return e;
+      a.n_wg = kFewGroups;
+      kernel<<<kFewGroups, 64 * NW, FK::lds, s>>>(a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (tiles) {
+      constexpr int NW = kPromptWaves;
+      typedef TileKernel<T, d.value, DV, NW, true> TK;
+      static std::atomic<uint64_t> done{0};
+      auto kernel = paged_tile_kernel<T, d.value, DV, NW>;
+      if ((e = raise_lds_limit((const void*)kernel, done, TK::lds)) != hipSuccess) return e;
+      a.n_wg = kTileGroups;
+      kernel<<<kTileGroups, 64 * NW, TK::lds, s>>>(a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      paged_join_kernel<T, DV, TK::BM><<<dim3(kTileGroups, 8), 256, 0, s>>>(a, a.tile_join, a.tile_part, a.tile_ml);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    paged_join_kernel<T, DV, kFewRows><<<dim3(kFewGroups, kFewRows / 4), 256, 0, s>>>(a, a.few_join, a.few_part, a.few_ml);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace moeq

@@ -1,0 +1,318 @@
+// Pieces shared by the attention kernels: types, the layout of key and value
+// tiles in LDS, and one wave's share of softmax(scale q k^T) v for 32 query
+// rows against blocks of 32 keys on the matrix cores.
+//
+// The products are taken transposed, S^T = K Q^T and O^T = V^T P^T
+// (v_mfma_f32_32x32x16): a lane then holds one query row (column lane % 32)
+// and, of a block of 32 keys, the 16 keys 8 (i / 4) + 4 (lane / 32) + i % 4.
+// A row's maximum and sum are sums over registers and one exchange between the
+// two halves of the wave, and the registers 8 s .. 8 s + 7 of S^T are, rounded,
+// the second operand of step s of the next product as they stand: the order of
+// the 16 keys of a step is free as long as V^T is read in the same one.
+#pragma once
+
+#include "internal.h"
+#include "layout.h"
+
+namespace moeq {
+
+namespace {
+
+#define MOEQ_LDS __attribute__((address_space(3)))
+
+typedef float f32x2v __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+
+// low, high: a dword's two values; kExponent: both exponent fields, and one of
+// their lowest bits each (a field of ones carries into the sign)
+struct Bf16 {
+  static constexpr uint32_t kExponent = 0x7F807F80u, kExponentStep = 0x00800080u;
+  static __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
+  static __device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+  static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+  }
+  // two values rounded to nearest even, the first in the low half
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v){lo, hi}, bf16x2));
+  }
+};
+
+struct F16 {
+  static constexpr uint32_t kExponent = 0x7C007C00u, kExponentStep = 0x04000400u;
+  static __device__ __forceinline__ float low(uint32_t v) { return (float)__builtin_bit_cast(f16x2, v)[0]; }
+  static __device__ __forceinline__ float high(uint32_t v) { return (float)__builtin_bit_cast(f16x2, v)[1]; }
+  static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                  0);
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v){lo, hi}, f16x2));
+  }
+};
+
+// ---- tiles in LDS ----
+// Rows of C 16-byte chunks follow each other (2 * C * 8 bytes a row).  Loads
+// straight into LDS place lane l's 16 bytes at 16 l, so a tile's layout is
+// chosen by which global chunk a lane asks for: chunk c of row r lies at chunk
+// swz(r, c) of that row, so that the 16 rows (K, ds_read_b128) or the 4 rows of
+// 64 bytes (V, ds_read_b64_tr_b16) that lanes read together fall on different
+// banks.  Rows come in granules of 16 (one page holds all of a granule).
+constexpr int kGranule = 16;
+
+template <int C>
+__device__ __forceinline__ int k_swz(int r, int c) {
+  if constexpr (C % 16 == 0)
+    return c ^ (r & 15);
+  else  // rows of 8 or 24 chunks: the row's parity already moves half the banks
+    return (c & ~7) | ((c ^ (r >> 1)) & 7);
+}
+template <int C>
+__device__ __forceinline__ int v_swz(int r, int c) {
+  if constexpr (C % 16 == 0)
+    return c ^ ((r & 3) << 2);
+  else
+    return c ^ (((r >> 1) & 1) << 2);
+}
+
+// 64 lanes' 16 bytes each from base + off (bytes) into LDS at dst + 16 * lane.
+// Written out because the compiler, given the builtin, waits for every load
+// in flight before each transposing LDS read.  There is no output register;
+// whoever reads the tile waits first (wait_loads).
+__device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_t dst) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(off), "s"(base), "s"(dst)
+      : "m0");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+// The lane's byte offsets of a granule's loads from its first row: load i
+// covers the granule's chunks 64 i .. 64 i + 63.
+template <int C, bool IsK>
+struct GranuleOffsets {
+  static constexpr int N = C / 4;  // loads per granule
+  uint32_t off[N];
+  __device__ __forceinline__ void set(uint32_t row_bytes, int last_row) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int s = i * 64 + lane, r = s / C, c = s % C;
+      off[i] = (uint32_t)min(r, last_row) * row_bytes + (uint32_t)(IsK ? k_swz<C>(r, c) : v_swz<C>(r, c)) * 16u;
+    }
+  }
+  __device__ __forceinline__ void load(const char* base, uint32_t dst) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) load_lds(base, off[i], dst + 1024u * i);
+  }
+};
+
+__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(MOEQ_LDS char*)p; }
+
+__device__ __forceinline__ u32x4 lds_read16(uint32_t a) { return *(const MOEQ_LDS u32x4*)(uintptr_t)a; }
+// Lane l of a group of 16 gets column l of the 4 rows x 16 columns whose row y
+// the group's lanes 4 y .. 4 y + 3 point at.
+__device__ __forceinline__ u32x2 lds_read_tr(uint32_t a) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MOEQ_LDS s16x4*)(uintptr_t)a));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// f(v of this lane, v of the lane 32 away)
+__device__ __forceinline__ float max_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+constexpr float kLowest = -3.40282347e38f;
+
+// One wave's state for 32 query rows; the lane's row is lane % 32.
+template <typename T, int D, int DV>
+struct RowBlock {
+  static constexpr int KS = D / 16;    // steps of the first product
+  static constexpr int DB = DV / 32;   // blocks of 32 value columns
+  static constexpr int KC = D / 8, VC = DV / 8;  // chunks per row
+  u32x4 q[KS];
+  f32x16 o[DB];
+  float m;      // the maximum that the exponents are taken against (raw scores), kLowest: no key yet
+  float neg_mc; // -m * c, 0 while there is no key
+  float l;      // this lane's share of the row's sum (its half of the keys)
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
+    m = kLowest;
+    neg_mc = 0.0f;
+    l = 0.0f;
+  }
+
+  // row: the lane's query row, null for none (zeros)
+  __device__ __forceinline__ void load_q(const char* row) {
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[s] = row ? *gptr((const u32x4*)(row + (2 * s + h) * 16)) : u32x4{0, 0, 0, 0};
+  }
+
+  // the lane's LDS offsets inside a tile whose first row is a multiple of 16
+  struct Addr {
+    uint32_t k[KS], v[DB];
+    __device__ __forceinline__ void set() {
+      const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) k[s] = (uint32_t)(r * KC + k_swz<KC>(r, 2 * s + h)) * 16u;
+      const int y = (lane >> 2) & 3, row = 4 * h + y;
+      // bytes within a block's 64: the group's half, the lane's 4 columns
+      const int within = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+        v[b] = (uint32_t)(row * VC + v_swz<VC>(row, 4 * b + (within >> 4))) * 16u + (uint32_t)(within & 15);
+    }
+  };
+
+  // scores of the 32 keys at LDS address kt
+  __device__ __forceinline__ f32x16 scores(const Addr& a, uint32_t kt) const {
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) s = T::mma(lds_read16(kt + a.k[t]), q[t], s);
+    return s;
+  }
+
+  // keys first + .. of a block: those outside [lo, hi) do not count
+  static __device__ __forceinline__ void mask(f32x16& s, int first, int lo, int hi) {
+    const int h = (threadIdx.x >> 5) & 1;
+    const uint32_t span = (uint32_t)max(hi - lo, 0);
+    const int at = first + 4 * h - lo;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      s[i] = (uint32_t)(at + 8 * (i / 4) + i % 4) < span ? s[i] : -INFINITY;
+  }
+
+  // c = scale * log2(e).  The rows' running maximum moves only where a score
+  // passes it by more than 2^kSlack in the exponential: the quotient O / l is
+  // the same for any m, sums and P stay in range, and the 16 DB multiplications
+  // of a rescale are rare.  Rounds P to T for the matrix cores; l sums the
+  // values before that rounding.
+  static constexpr float kSlack = 8.0f;
+  template <int NB>
+  __device__ __forceinline__ void softmax(f32x16 (&s)[NB], float c, uint32_t (&p)[NB][8]) {
+    float t = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t = fmaxf(t, s[b][i]);
+    t = max_halves(t);
+    if (__any(fmaf(t, c, neg_mc) > kSlack || (m == kLowest && t > kLowest))) {
+      const float mn = fmaxf(m, t);
+      const float nmc = mn == kLowest ? 0.0f : -mn * c;
+      const float f = m == kLowest ? 0.0f : exp2_fast(nmc - neg_mc);
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] *= f;
+      l *= f;
+      m = mn;
+      neg_mc = nmc;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float x = exp2_fast(fmaf(s[b][i], c, neg_mc)), y = exp2_fast(fmaf(s[b][i + 1], c, neg_mc));
+        l += x;
+        l += y;
+        p[b][i / 2] = T::pack(x, y);
+      }
+  }
+
+  // o += P V for the 32 keys at LDS address vt.  With MASKED and `finite`,
+  // infinities and NaN of V count as zeros.
+  template <bool MASKED = false>
+  __device__ __forceinline__ void values(const Addr& a, uint32_t vt, const uint32_t (&p)[8], bool finite = false) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const u32x4 pb = {p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]};
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const u32x2 x = lds_read_tr(vt + a.v[b] + (16 * t) * VC * 16);
+        const u32x2 y = lds_read_tr(vt + a.v[b] + (16 * t + 8) * VC * 16);
+        u32x4 v = {x.x, x.y, y.x, y.y};
+        if (MASKED && finite)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] &= ~nonfinite(v[j]);
+        o[b] = T::mma(v, pb, o[b]);
+      }
+    }
+  }
+
+  // A key that a row does not see has weight 0 there, and 0 times an infinity
+  // or NaN must not reach the row.  Where some row of a block does not see some
+  // key and the block's values are not all finite (any_nonfinite), the product
+  // takes only the finite ones, and those rows that do see the others get them
+  // at the end (add_nonfinite): an infinity of any positive weight is one.
+  // all ones in the halves of v that hold an infinity or NaN
+  static __device__ __forceinline__ uint32_t nonfinite(uint32_t v) {
+    const uint32_t m = ((v & T::kExponent) + T::kExponentStep) & 0x80008000u;
+    return (m - (m >> 15)) | m;
+  }
+  // whether a value of the 32 keys at vt is infinite or NaN
+  static __device__ __forceinline__ bool any_nonfinite(uint32_t vt) {
+    const int lane = threadIdx.x & 63;
+    uint32_t f = 0;
+#pragma unroll 1
+    for (int i = 0; i < DV / 16; ++i) {
+      const u32x4 x = lds_read16(vt + (uint32_t)(i * 64 + lane) * 16u);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f |= nonfinite(x[j]);
+    }
+    return __any(f != 0);
+  }
+
+  // keys first .. end - 1, whose value rows value_row(key) points at (global);
+  // the lane's row sees [lo, hi)
+  template <typename F>
+  __device__ __forceinline__ void add_nonfinite(int first, int end, int lo, int hi, F value_row) {
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int c = 0; c < 4 * DB; ++c) {  // columns 8 c + 4 h .. + 3
+      float e[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+      for (int key = first; key < end; ++key) {
+        const u32x2 v = *gptr((const u32x2*)(value_row(key) + 16 * c + 8 * h));
+        const bool seen = key >= lo && key < hi;
+        const uint32_t f0 = seen ? nonfinite(v.x) : 0u, f1 = seen ? nonfinite(v.y) : 0u;
+        e[0] += f0 & 0xFFFFu ? T::low(v.x) : 0.0f;
+        e[1] += f0 >> 16 ? T::high(v.x) : 0.0f;
+        e[2] += f1 & 0xFFFFu ? T::low(v.y) : 0.0f;
+        e[3] += f1 >> 16 ? T::high(v.y) : 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[c / 4][4 * (c % 4) + j] += e[j];
+    }
+  }
+};
+
+}  // namespace
+
+}  // namespace moeq

@@ -31,6 +31,7 @@ MOEQ_PROJ_GATE, MOEQ_PROJ_UP, MOEQ_PROJ_DOWN = 0, 1, 2
 MOEQ_WEIGHTS_HOST, MOEQ_WEIGHTS_DEVICE = 0, 1
 MOEQ_PATH_AUTO, MOEQ_PATH_DECODE, MOEQ_PATH_PREFILL = 0, 1, 2
 MOEQ_DECODER_EXACT, MOEQ_DECODER_GEMV_SUBNORMAL, MOEQ_DECODER_GEMM_F16 = 0, 1, 2
+MOEQ_BF16, MOEQ_F16 = 0, 1
 
 
 class MoeqError(RuntimeError):
@@ -74,6 +75,23 @@ class moeq_plan_report(ctypes.Structure):
                 ("n_rule3", ctypes.c_int32), ("feasible", ctypes.c_int32)]
 
 
+class moeq_attn(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("value_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class moeq_rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class moeq_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("k_page_stride", ctypes.c_int64), ("k_slot_stride", ctypes.c_int64),
+                ("k_head_stride", ctypes.c_int64), ("v_page_stride", ctypes.c_int64),
+                ("v_slot_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build()")
@@ -85,7 +103,8 @@ def _load():
     except ImportError:
         pass
     lib = ctypes.CDLL(LIB_PATH)
-    P, I32, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
+    P, I32, I64, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    ATTN, ROWS, CACHE = (ctypes.POINTER(c) for c in (moeq_attn, moeq_rows, moeq_kv_cache))
     sig = {
         "moeq_layer_create": [ctypes.POINTER(moeq_config), P, P, P, P, I32, ctypes.POINTER(P)],
         "moeq_forward": [P, P, P, I32, P, P],
@@ -109,6 +128,11 @@ def _load():
                                    P, P, P, P],
         "moeq_expert_importance_noalloc": [ctypes.POINTER(moeq_config), P, P, I32, ctypes.c_double,
                                            ctypes.c_double, P, P, P, P],
+        "moeq_kv_plan": [P, P, I32, P, I64, I32, P, I32, P, P, I32, I32, P, P, P, P, P],
+        "moeq_kv_append": [ATTN, CACHE, ROWS, ROWS, P, I32, P],
+        "moeq_attn_prompt": [ATTN, ROWS, ROWS, ROWS, P, I32, I32, ROWS, P, P],
+        "moeq_attn_paged": [ATTN, ROWS, CACHE, P, P, P, I64, I32, I32, I32, I32, ROWS, P, P, ctypes.c_uint64, P],
+        "moeq_attn_paged_workspace": [ATTN, I32, ctypes.POINTER(ctypes.c_uint64)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -258,6 +282,37 @@ def moeq_expert_importance_noalloc(cfg, score_bias, logits, n_tokens, alpha, ret
     """As moeq_expert_importance, with the library's static scratch (no allocation)."""
     _check(lib.moeq_expert_importance_noalloc(ctypes.byref(cfg), score_bias or None, logits, n_tokens, alpha,
                                               retain, importance, mask, counts or None, stream or None))
+
+
+def moeq_kv_plan(ctx_lens, new_lens, n_requests, block_table, table_stride, max_blocks, free_pages, n_pages, pool_in,
+                 pool_out, page_size, n_tokens, cu_q, kv_lens, slots, positions, stream=0):
+    """Every array a device address."""
+    _check(lib.moeq_kv_plan(ctx_lens, new_lens, n_requests, block_table, table_stride, max_blocks, free_pages, n_pages,
+                            pool_in, pool_out, page_size, n_tokens, cu_q, kv_lens, slots, positions, stream or None))
+
+
+def moeq_kv_append(attn, cache, k, v, slots, n_tokens, stream=0):
+    """attn: moeq_attn; cache: moeq_kv_cache; k, v: moeq_rows; slots: device address."""
+    _check(lib.moeq_kv_append(attn, cache, k, v, slots, n_tokens, stream or None))
+
+
+def moeq_attn_prompt(attn, q, k, v, cu, n_seqs, n_tokens, out, lse=0, stream=0):
+    """attn: moeq_attn; q, k, v, out: moeq_rows; cu, lse: device addresses (lse may be 0)."""
+    _check(lib.moeq_attn_prompt(attn, q, k, v, cu, n_seqs, n_tokens, out, lse or None, stream or None))
+
+
+def moeq_attn_paged(attn, q, cache, cu_q, kv_lens, block_table, table_stride, max_blocks, n_requests, n_tokens, max_new,
+                    out, lse, workspace, workspace_bytes, stream=0):
+    """attn: moeq_attn; cache: moeq_kv_cache; q, out: moeq_rows; the rest device addresses (lse may be 0)."""
+    _check(lib.moeq_attn_paged(attn, q, cache, cu_q, kv_lens, block_table, table_stride, max_blocks, n_requests,
+                               n_tokens, max_new, out, lse or None, workspace, workspace_bytes, stream or None))
+
+
+def moeq_attn_paged_workspace(attn, max_new):
+    """Bytes of moeq_attn_paged's workspace."""
+    b = ctypes.c_uint64()
+    _check(lib.moeq_attn_paged_workspace(attn, max_new, ctypes.byref(b)))
+    return b.value
 
 
 def expert_importance(shape, logits, *, alpha, retain, bias=None, stream=None):

@@ -1,0 +1,97 @@
+"""Argument checks of the cache and attention entry points, on a machine without
+a GPU: each refusal comes before any HIP call."""
+import ctypes
+
+import pytest
+
+moeq = pytest.importorskip("paper_2509_25689_amd.moeq")
+L = moeq.lib
+BAD, UNSUP, CAP = moeq.MOEQ_ERR_INVALID_ARG, moeq.MOEQ_ERR_UNSUPPORTED, moeq.MOEQ_ERR_CAPACITY
+FAKE = 4096   # never dereferenced: validation fails first
+
+
+def _attn(**kw):
+    a = moeq.moeq_attn(8, 2, 128, 128, moeq.MOEQ_BF16, 1, 0, 0.1)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def _rows(p=FAKE, t=1024, h=128):
+    return moeq.moeq_rows(p, t, h)
+
+
+def _cache(**kw):
+    c = moeq.moeq_kv_cache(FAKE, FAKE, 10, 64, 16384, 128, 8192, 16384, 128, 8192)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def _prompt(a=None, q=None, k=None, v=None, cu=FAKE, seqs=1, tokens=8, out=None, lse=None):
+    return L.moeq_attn_prompt(a or _attn(), q or _rows(), k or _rows(), v or _rows(), cu, seqs, tokens, out or _rows(), lse, None)
+
+
+def _paged(a=None, q=None, c=None, cu=FAKE, kv=FAKE, table=FAKE, stride=8, blocks=8, reqs=1, tokens=1, new=1, out=None,
+           lse=None, ws=FAKE, size=1 << 40):
+    return L.moeq_attn_paged(a or _attn(), q or _rows(), c or _cache(), cu, kv, table, stride, blocks, reqs, tokens, new,
+                             out or _rows(), lse, ws, size, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n_kv_heads=0), BAD), (dict(n_heads=7), BAD), (dict(n_heads=0), BAD), (dict(n_heads=1024, n_kv_heads=2), BAD),
+    (dict(dtype=2), BAD), (dict(head_dim=0), BAD), (dict(causal=2), BAD), (dict(window=-1), BAD),
+    (dict(window=3, causal=0), BAD), (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD), (dict(scale=float("nan")), BAD),
+    (dict(scale=float("inf")), BAD), (dict(head_dim=96), UNSUP), (dict(head_dim=64), UNSUP), (dict(value_dim=192), UNSUP)])
+def test_attention_description(kw, status):
+    assert _prompt(_attn(**kw)) == status and moeq.moeq_last_error()
+    assert _paged(_attn(**kw)) == status
+    b = ctypes.c_uint64()
+    assert L.moeq_attn_paged_workspace(_attn(**kw), 1, ctypes.byref(b)) == status
+
+
+def test_prompt_arguments():
+    assert L.moeq_attn_prompt(None, _rows(), _rows(), _rows(), FAKE, 1, 1, _rows(), None, None) == BAD
+    assert L.moeq_attn_prompt(_attn(), None, _rows(), _rows(), FAKE, 1, 1, _rows(), None, None) == BAD
+    for name in ("q", "k", "v", "out"):
+        for r in (_rows(p=None), _rows(p=FAKE + 8), _rows(t=12), _rows(h=4), _rows(t=-8)):
+            assert _prompt(**{name: r}) == BAD, name
+            assert name in moeq.moeq_last_error()
+    assert _prompt(k=_rows(t=1 << 26)) == BAD
+    assert _prompt(cu=None) == BAD and _prompt(cu=FAKE + 2) == BAD and _prompt(lse=FAKE + 1) == BAD
+    assert _prompt(seqs=-1) == BAD and _prompt(tokens=-1) == BAD and _prompt(tokens=(1 << 24) + 1) == BAD
+    assert _prompt(_attn(n_heads=256, n_kv_heads=256), tokens=1 << 24) == UNSUP
+    assert _prompt(seqs=0) == moeq.MOEQ_OK and _prompt(tokens=0) == moeq.MOEQ_OK   # nothing to do
+
+
+def test_paged_arguments():
+    for kw in (dict(k=None), dict(v=FAKE + 8), dict(page_size=24), dict(page_size=8), dict(page_size=8192), dict(n_pages=0),
+               dict(n_pages=1 << 26), dict(k_page_stride=4), dict(v_head_stride=-8), dict(k_slot_stride=1 << 26)):
+        assert _paged(c=_cache(**kw)) == BAD, kw
+    assert _paged(blocks=0) == BAD and _paged(stride=7) == BAD
+    assert _paged(cu=None) == BAD and _paged(kv=None) == BAD and _paged(table=FAKE + 1) == BAD
+    assert _paged(ws=None) == BAD and _paged(ws=FAKE + 16) == BAD
+    assert _paged(new=-1) == BAD and _paged(reqs=-1) == BAD
+    need = moeq.moeq_attn_paged_workspace(_attn(), 1)
+    assert _paged(size=need - 1) == CAP and str(need) in moeq.moeq_last_error()
+    assert moeq.moeq_attn_paged_workspace(_attn(), 100) > need
+    assert _paged(reqs=0) == moeq.MOEQ_OK and _paged(tokens=0) == moeq.MOEQ_OK
+
+
+def test_plan_arguments():
+    names = ["ctx", "new", "R", "table", "stride", "blocks", "free", "pages", "pool", "out", "P", "T", "cu", "kv", "slots",
+             "pos", "stream"]
+    good = dict(zip(names, [FAKE, FAKE, 4, FAKE, 8, 8, FAKE, 100, FAKE, FAKE, 16, 4, FAKE, FAKE, FAKE, FAKE, None]))
+    for kw in (dict(ctx=None), dict(new=None), dict(table=None), dict(free=None), dict(pool=None), dict(out=None),
+               dict(cu=None), dict(kv=None), dict(slots=None), dict(pos=None), dict(R=-1), dict(T=-1), dict(P=20),
+               dict(pages=0), dict(blocks=0), dict(stride=4), dict(cu=FAKE + 2), dict(blocks=1 << 28, stride=1 << 28)):
+        assert L.moeq_kv_plan(*{**good, **kw}.values()) == BAD, kw
+
+
+def test_append_arguments():
+    def call(a=None, c=None, k=None, v=None, slots=FAKE, T=4):
+        return L.moeq_kv_append(a or _attn(), c or _cache(), k or _rows(), v or _rows(), slots, T, None)
+    assert call(_attn(head_dim=12)) == BAD and call(_attn(value_dim=2048)) == BAD
+    assert call(c=_cache(page_size=5)) == BAD and call(k=_rows(p=None)) == BAD and call(v=_rows(t=3)) == BAD
+    assert call(slots=None) == BAD and call(T=-1) == BAD
+    assert call(T=0) == moeq.MOEQ_OK
