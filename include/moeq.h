@@ -501,7 +501,7 @@ typedef struct {
  * do not fit max_blocks, or which needs pages and the pages needed up to and
  * with it exceed those free at the step's start, is refused: it takes none, its
  * slots are -1 and its kv_len 0; the others are served.
- *   ctx_lens, new_lens  DEVICE int32 [n_requests]
+ *   ctx_lens, new_lens  DEVICE int32 [n_requests], at most 2^30
  *   block_table  DEVICE int32 [n_requests x max_blocks], rows table_stride
  *                apart; the entries of pages taken are written
  *   free_pages   DEVICE int32 [n_pages], the ring; pages given back are written

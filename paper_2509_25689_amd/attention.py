@@ -18,58 +18,68 @@ import torch
 from . import moeq
 
 _DTYPES = {torch.bfloat16: moeq.MOEQ_BF16, torch.float16: moeq.MOEQ_F16}
+_INT = torch.int32
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _fail(name, what, t):
-    raise ValueError(f"{name} must {what}, got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
-
-
-def _tensor(name, t, dtype, dims, device):
+# A step's calls are short on the GPU, so each check is a few comparisons; the
+# message is put together only where one fails.
+def _refuse(name, t, dtype, shape, device, what=None):
+    """Raises for the first thing that is wrong with a tensor (None in `shape`: any size)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.device.type != "cuda" or (device is not None and t.device != device):
-        _fail(name, f"be on {device or 'a GPU'}", t)
-    if t.dtype != dtype:
-        _fail(name, f"be {dtype}", t)
-    if t.dim() != dims:
-        _fail(name, f"have {dims} dimensions", t)
+    if t.get_device() != device:
+        what = f"be on cuda:{device}"
+    elif t.dtype != dtype:
+        what = f"be {dtype}"
+    elif t.dim() != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)):
+        what = f"have shape {tuple('any' if n is None else n for n in shape)}"
+    raise ValueError(f"{name} must {what or 'have a dense last dimension'}, got {tuple(t.shape)} {t.dtype} on {t.device}, "
+                     f"strides {t.stride()}")
 
 
-def _ints(name, t, shape, device):
-    """An int32 tensor whose last dimension is dense; None in `shape`: any size."""
-    _tensor(name, t, torch.int32, len(shape), device)
-    for have, want in zip(t.shape, shape):
-        if want is not None and have != want:
-            _fail(name, f"have shape {tuple(shape)}", t)
-    if t.stride(-1) != 1 and t.shape[-1] > 1 or (t.dim() == 1 and not t.is_contiguous()):
-        _fail(name, "have a dense last dimension", t)
+def _ints(name, t, n, device):
+    """The address of an int32 vector of n."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is _INT and t.get_device() == device and t.shape == (n,)
+            and t.is_contiguous()):
+        _refuse(name, t, _INT, (n,), device)
+    return t.data_ptr()
+
+
+def _table(t, n, device):
+    """(address, row stride, columns) of a block table of n rows."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is _INT and t.get_device() == device and t.dim() == 2
+            and t.shape[0] == n and (t.shape[1] <= 1 or t.stride(1) == 1)):
+        _refuse("block_table", t, _INT, (n, None), device)
+    w = t.shape[1]
+    return t.data_ptr(), t.stride(0) if n > 1 else w, w
 
 
 def _rows(name, t, dtype, shape, device):
     """A moeq_rows of a tensor [tokens, heads, dim]."""
-    _tensor(name, t, dtype, 3, device)
-    n, h, d = t.shape
-    if (n, h, d) != shape:
-        _fail(name, f"have shape {shape}", t)
-    s = t.stride()
-    if s[2] != 1:
-        _fail(name, "have a dense last dimension", t)
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape):
+        _refuse(name, t, dtype, shape, device)
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        _refuse(name, t, dtype, shape, device)
     # the stride of a dimension of one element says nothing
-    return moeq.moeq_rows(t.data_ptr(), s[0] if n > 1 else 0, s[1] if h > 1 else 0)
+    return moeq.moeq_rows(t.data_ptr(), s0 if shape[0] > 1 else 0, s1 if shape[1] > 1 else 0)
 
 
 def _cache(k, v, dtype, device):
-    _tensor("k_cache", k, dtype, 4, device)
-    _tensor("v_cache", v, dtype, 4, device)
-    if k.shape[:3] != v.shape[:3]:
-        _fail("v_cache", f"have k_cache's pages, places and heads {tuple(k.shape[:3])}", v)
-    if k.stride(3) != 1 or v.stride(3) != 1:
-        _fail("k_cache and v_cache", "have a dense last dimension", k)
-    ks, vs = k.stride(), v.stride()
-    one = k.shape[0] > 1, True, k.shape[2] > 1
-    return moeq.moeq_kv_cache(k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[1],
-                              ks[0] if one[0] else 0, ks[1], ks[2] if one[2] else 0,
-                              vs[0] if one[0] else 0, vs[1], vs[2] if one[2] else 0)
+    for name, t, shape in (("k_cache", k, (None,) * 4), ("v_cache", v, None)):
+        shape = shape or (*k.shape[:3], None)
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.dim() == 4
+                and t.shape[:3] == k.shape[:3] and t.stride(3) == 1):
+            _refuse(name, t, dtype, shape, device)
+    n, places, heads, _ = k.shape
+    kp, ks, kh, _ = k.stride()
+    vp, vs, vh, _ = v.stride()
+    if n == 1:
+        kp = vp = 0
+    if heads == 1:
+        kh = vh = 0
+    return moeq.moeq_kv_cache(k.data_ptr(), v.data_ptr(), n, places, kp, ks, kh, vp, vs, vh)
 
 
 def _attn(heads, kv_heads, dim, value_dim, dtype, causal=True, window=0, scale=None):
@@ -80,28 +90,30 @@ def _attn(heads, kv_heads, dim, value_dim, dtype, causal=True, window=0, scale=N
                           dim ** -0.5 if scale is None else scale)
 
 
-class _On:
-    """The device and stream of a call: `device` current, new tensors usable on the stream."""
+def _on(name, t, dims, stream):
+    """(device index, stream, the stream as torch's where it is not the current
+    one) of a call whose first tensor is t, of `dims` dimensions."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a tensor on a GPU")
+    device = t.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device} but cuda:{torch.cuda.current_device()} is current")
+    if t.dim() != dims:
+        _refuse(name, t, t.dtype, (None,) * dims, device)
+    current = _raw_stream(device)
+    if stream is None or stream == current:
+        return device, current, None
+    return device, stream, torch.cuda.ExternalStream(stream, device=device)
 
-    def __init__(self, device, stream):
-        current = torch.cuda.current_stream(device).cuda_stream
-        self.device, self.stream = device, current if stream is None else stream
-        self.other = None if self.stream == current else torch.cuda.ExternalStream(self.stream, device=device)
 
-    def empty(self, shape, dtype):
-        t = torch.empty(shape, dtype=dtype, device=self.device)
-        if self.other is not None:
-            # the memory may still be in use on the current stream, where it was last freed
-            self.other.wait_stream(torch.cuda.current_stream(self.device))
-            t.record_stream(self.other)
-        return t
-
-
-def _guard(t):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
-        raise TypeError("tensors must be on a GPU")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {t.device} but cuda:{torch.cuda.current_device()} is current")
+def _new(like, shape, dtype, other):
+    """A new tensor for the call's stream."""
+    t = torch.empty(shape, dtype=dtype, device=like.device)
+    if other is not None:
+        # the memory may still be in use on the current stream, where it was last freed
+        other.wait_stream(torch.cuda.current_stream(like.device))
+        t.record_stream(other)
+    return t
 
 
 def empty_cache(n_pages, page_size, kv_heads, dim, value_dim=None, *, dtype=torch.bfloat16, layout="hnd", device="cuda"):
@@ -129,41 +141,33 @@ def plan(ctx_lens, new_lens, block_table, free_pages, pool, *, page_size, n_toke
     -> (cu_q [R + 1], kv_lens [R], slots [n_tokens], positions [n_tokens],
     block_table, free_pages, pool_out [3]: head, pages free, requests refused).
     pool_out: a new tensor by default; may be `pool` itself."""
-    _guard(ctx_lens)
-    dev = ctx_lens.device
-    R = ctx_lens.shape[0] if ctx_lens.dim() == 1 else -1
-    _ints("ctx_lens", ctx_lens, (R,), dev)
-    _ints("new_lens", new_lens, (R,), dev)
-    _ints("block_table", block_table, (R, None), dev)
-    _ints("free_pages", free_pages, (None,), dev)
-    _ints("pool", pool, (3,), dev)
-    on = _On(dev, stream)
+    dev, stream, other = _on("ctx_lens", ctx_lens, 1, stream)
+    R = ctx_lens.shape[0]
+    if n_tokens < 0:
+        raise ValueError(f"n_tokens must not be negative, got {n_tokens}")
+    n_pages = free_pages.shape[0]
+    # one allocation for what the step returns
+    cu, lens, slots, positions, own = _new(ctx_lens, 2 * R + 2 * n_tokens + 4, _INT, other).split_with_sizes(
+        (R + 1, R, n_tokens, n_tokens, 3))
     if pool_out is None:
-        pool_out = on.empty(3, torch.int32)
-    _ints("pool_out", pool_out, (3,), dev)
-    cu, lens = on.empty(R + 1, torch.int32), on.empty(R, torch.int32)
-    slots, positions = on.empty(n_tokens, torch.int32), on.empty(n_tokens, torch.int32)
-    moeq.moeq_kv_plan(ctx_lens.data_ptr(), new_lens.data_ptr(), R, block_table.data_ptr(),
-                      block_table.stride(0) if R > 1 else block_table.shape[1], block_table.shape[1],
-                      free_pages.data_ptr(), free_pages.shape[0], pool.data_ptr(), pool_out.data_ptr(), page_size,
-                      n_tokens, cu.data_ptr(), lens.data_ptr(), slots.data_ptr(), positions.data_ptr(), on.stream)
+        pool_out = own
+    table, stride, blocks = _table(block_table, R, dev)
+    moeq.moeq_kv_plan(_ints("ctx_lens", ctx_lens, R, dev), _ints("new_lens", new_lens, R, dev), R, table, stride, blocks,
+                      _ints("free_pages", free_pages, n_pages, dev), n_pages, _ints("pool", pool, 3, dev),
+                      _ints("pool_out", pool_out, 3, dev), page_size, n_tokens, cu.data_ptr(), lens.data_ptr(),
+                      slots.data_ptr(), positions.data_ptr(), stream)
     return cu, lens, slots, positions, block_table, free_pages, pool_out
 
 
 def append(k_cache, v_cache, k, v, slots, *, stream=None):
     """Stores k [T, kv heads, dim] and v [T, kv heads, value dim] in the cache's
     slots [T] (int32; those outside the cache are skipped)."""
-    _guard(k)
-    dev = k.device
-    c = _cache(k_cache, v_cache, k.dtype, dev)
-    T, heads = k.shape[0], k_cache.shape[2]
-    kr = _rows("k", k, k.dtype, (T, heads, k_cache.shape[3]), dev)
-    vr = _rows("v", v, k.dtype, (T, heads, v_cache.shape[3]), dev)
-    _ints("slots", slots, (T,), dev)
-    if stream is None:
-        stream = torch.cuda.current_stream(dev).cuda_stream
-    moeq.moeq_kv_append(_attn(heads, heads, k_cache.shape[3], v_cache.shape[3], k.dtype), c, kr, vr, slots.data_ptr(), T,
-                        stream)
+    dev, stream, _ = _on("k", k, 3, stream)
+    dt = k.dtype
+    c = _cache(k_cache, v_cache, dt, dev)
+    T, (_, _, heads, dim), value_dim = k.shape[0], k_cache.shape, v_cache.shape[3]
+    moeq.moeq_kv_append(_attn(heads, heads, dim, value_dim, dt), c, _rows("k", k, dt, (T, heads, dim), dev),
+                        _rows("v", v, dt, (T, heads, value_dim), dev), _ints("slots", slots, T, dev), T, stream)
 
 
 def prompt(q, k, v, cu_seqlens, *, causal=True, window=0, scale=None, out=None, return_lse=False, stream=None):
@@ -171,23 +175,23 @@ def prompt(q, k, v, cu_seqlens, *, causal=True, window=0, scale=None, out=None, 
     v [T, kv heads, value dim], cu_seqlens int32 [sequences + 1].
     -> out [T, heads, value dim], with return_lse also lse float32 [T, heads].
     scale: dim ** -0.5 by default."""
-    _guard(q)
-    dev, dt = q.device, q.dtype
-    _tensor("q", q, dt, 3, dev)
-    _tensor("k", k, dt, 3, dev)
-    _tensor("v", v, dt, 3, dev)
-    (T, heads, dim), kv_heads, value_dim = q.shape, k.shape[1], v.shape[2]
+    dev, stream, other = _on("q", q, 3, stream)
+    dt, (T, heads, dim) = q.dtype, q.shape
+    for name, t in (("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            _refuse(name, t, dt, (T, None, None), dev)
+    kv_heads, value_dim = k.shape[1], v.shape[2]
     a = _attn(heads, kv_heads, dim, value_dim, dt, causal, window, scale)
-    _ints("cu_seqlens", cu_seqlens, (None,), dev)
-    qr, kr = _rows("q", q, dt, (T, heads, dim), dev), _rows("k", k, dt, (T, kv_heads, dim), dev)
-    vr = _rows("v", v, dt, (T, kv_heads, value_dim), dev)
-    on = _On(dev, stream)
+    shape = (T, heads, value_dim)
+    n = cu_seqlens.shape[0]
+    if n < 1:
+        raise ValueError("cu_seqlens must hold at least one element")
+    args = (_rows("q", q, dt, (T, heads, dim), dev), _rows("k", k, dt, (T, kv_heads, dim), dev),
+            _rows("v", v, dt, (T, kv_heads, value_dim), dev), _ints("cu_seqlens", cu_seqlens, n, dev))
     if out is None:
-        out = on.empty((T, heads, value_dim), dt)
-    lse = on.empty((T, heads), torch.float32) if return_lse else None
-    moeq.moeq_attn_prompt(a, qr, kr, vr, cu_seqlens.data_ptr(), cu_seqlens.shape[0] - 1, T,
-                          _rows("out", out, dt, (T, heads, value_dim), dev), 0 if lse is None else lse.data_ptr(),
-                          on.stream)
+        out = _new(q, shape, dt, other)
+    lse = _new(q, (T, heads), torch.float32, other) if return_lse else None
+    moeq.moeq_attn_prompt(a, *args, n - 1, T, _rows("out", out, dt, shape, dev), lse.data_ptr() if return_lse else 0, stream)
     return (out, lse) if return_lse else out
 
 
@@ -198,33 +202,27 @@ def paged(q, k_cache, v_cache, cu_q, kv_lens, block_table, *, max_new, causal=Tr
     q [T, heads, dim] -> out [T, heads, value dim], with return_lse also lse
     float32 [T, heads].  max_new: at least the most new tokens of a request.
     workspace: a uint8 tensor of paged_workspace(..) bytes, else made here."""
-    _guard(q)
-    dev, dt = q.device, q.dtype
-    _tensor("q", q, dt, 3, dev)
+    dev, stream, other = _on("q", q, 3, stream)
+    dt, (T, heads, dim) = q.dtype, q.shape
     c = _cache(k_cache, v_cache, dt, dev)
-    (T, heads, dim), kv_heads, value_dim = q.shape, k_cache.shape[2], v_cache.shape[3]
+    kv_heads, value_dim = k_cache.shape[2], v_cache.shape[3]
     if k_cache.shape[3] != dim:
-        _fail("k_cache", f"have keys of q's {dim}", k_cache)
+        _refuse("k_cache", k_cache, dt, (None, None, None, dim), dev)
     a = _attn(heads, kv_heads, dim, value_dim, dt, causal, window, scale)
-    R = kv_lens.shape[0]
-    _ints("kv_lens", kv_lens, (R,), dev)
-    _ints("cu_q", cu_q, (R + 1,), dev)
-    _ints("block_table", block_table, (R, None), dev)
-    qr = _rows("q", q, dt, (T, heads, dim), dev)
-    on = _On(dev, stream)
-    if out is None:
-        out = on.empty((T, heads, value_dim), dt)
-    lse = on.empty((T, heads), torch.float32) if return_lse else None
+    shape, R = (T, heads, value_dim), kv_lens.shape[0]
+    table, stride, blocks = _table(block_table, R, dev)
+    args = (_rows("q", q, dt, (T, heads, dim), dev), c, _ints("cu_q", cu_q, R + 1, dev), _ints("kv_lens", kv_lens, R, dev),
+            table, stride, blocks, R, T, max_new)
     if workspace is None:
-        workspace = on.empty(moeq.moeq_attn_paged_workspace(a, max_new), torch.uint8)
-    else:
-        _tensor("workspace", workspace, torch.uint8, 1, dev)
-        if not workspace.is_contiguous():
-            _fail("workspace", "be contiguous", workspace)
-    moeq.moeq_attn_paged(a, qr, c, cu_q.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr(),
-                         block_table.stride(0) if R > 1 else block_table.shape[1], block_table.shape[1], R, T, max_new,
-                         _rows("out", out, dt, (T, heads, value_dim), dev), 0 if lse is None else lse.data_ptr(),
-                         workspace.data_ptr(), workspace.shape[0], on.stream)
+        workspace = _new(q, moeq.moeq_attn_paged_workspace(a, max_new), torch.uint8, other)
+    elif not (workspace.dtype is torch.uint8 and workspace.get_device() == dev and workspace.dim() == 1
+              and workspace.is_contiguous()):
+        _refuse("workspace", workspace, torch.uint8, (None,), dev)
+    if out is None:
+        out = _new(q, shape, dt, other)
+    lse = _new(q, (T, heads), torch.float32, other) if return_lse else None
+    moeq.moeq_attn_paged(a, *args, _rows("out", out, dt, shape, dev), lse.data_ptr() if return_lse else 0,
+                         workspace.data_ptr(), workspace.shape[0], stream)
     return (out, lse) if return_lse else out
 
 

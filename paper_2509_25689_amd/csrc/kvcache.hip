@@ -17,23 +17,24 @@ namespace moeq {
 
 namespace {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kMaxThreads = 1024;
 constexpr int kTokensPerGroup = 2048;
+constexpr int kMostLen = 1 << 30;  // longer lengths count as this
 
-struct Sums {
-  long long tokens, need, gone;
-};
-__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
-  return Sums{a.tokens + b.tokens, a.need + b.need, a.gone + b.gone};
+// Sums of non-negative numbers that stop at 2^31 - 1 (and so stay monotone)
+__device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int add_dpp(int v) {
+  return add_sat(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, false));
 }
-
-struct PlanShared {
-  // of each request of the chunk: exclusive sums, and what its tokens need
-  int tokens[kPlanThreads], need[kPlanThreads], gone[kPlanThreads];
-  int ctx[kPlanThreads], held[kPlanThreads];
-  uint8_t ok[kPlanThreads];
-  Sums wave[kPlanThreads / 64];
-};
+__device__ __forceinline__ int wave_incl_sat(int v) {
+  v = add_dpp<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v = add_dpp<0x112, 0xF>(v);
+  v = add_dpp<0x114, 0xF>(v);
+  v = add_dpp<0x118, 0xF>(v);
+  v = add_dpp<0x142, 0xA>(v);  // row_bcast 15, 31
+  return add_dpp<0x143, 0xC>(v);
+}
 
 // last i of n with v[i] <= x (v ascending, v[0] <= x)
 __device__ __forceinline__ int bisect(const int* v, int n, int x) {
@@ -46,113 +47,114 @@ __device__ __forceinline__ int bisect(const int* v, int n, int x) {
   return lo;
 }
 
+enum { kTokens, kNeed, kGone, kSums };
+
+template <int NT>
+struct PlanShared {
+  int excl[kSums][NT];        // of each request of the chunk: sums before it
+  int ctx[NT], held[NT];
+  uint8_t ok[NT];
+  int wave[kSums][NT / 64];
+  int refused;
+};
+
 // fill: write everything but pool_out; pool: write pool_out
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a, bool fill, bool pool) {
-  __shared__ PlanShared sh;
+template <int NT>
+__global__ __launch_bounds__(NT) void plan_kernel(PlanArgs a, bool fill, bool pool) {
+  __shared__ PlanShared<NT> sh;
+  constexpr int NW = NT / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t N = a.n_pages;
-  const uint32_t head = (uint32_t)a.pool_in[0] % N;
-  const int free0 = min(max(a.pool_in[1], 0), a.n_pages);
+  const uint32_t head_in = (uint32_t)a.pool_in[0], head = head_in < N ? head_in : head_in % N;
+  const int free0 = min(max(a.pool_in[1], 0), a.n_pages), room = a.n_pages - free0;
   const int P = 1 << a.page_shift;
   const bool first = blockIdx.x == 0;
-  const int step = gridDim.x * kPlanThreads, at = blockIdx.x * kPlanThreads + tid;
-  auto ring = [&](uint32_t i) { return i < N ? i : i - N; };
-  auto clip = [](long long v, int most) { return (int)(v < most ? v : most); };
-  Sums base{0, 0, 0};
-  long long taken = 0;
-  int refused = 0;
-  for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
-    const int r = r0 + tid, m = min(kPlanThreads, a.R - r0);
+  const int step = gridDim.x * NT, at = blockIdx.x * NT + tid;
+  auto ring = [&](int i) { return (uint32_t)i + head < N ? i + head : i + head - N; };  // 0 <= i < N
+  int base[kSums] = {0, 0, 0}, taken = 0;
+  if (tid == 0) sh.refused = 0;
+  for (int r0 = 0; r0 < a.R; r0 += NT) {
+    const int r = r0 + tid, m = min(NT, a.R - r0);
     int ctx = 0, add = 0;
     if (r < a.R) {
-      ctx = max(a.ctx[r], 0);
-      add = a.add[r];
+      ctx = min(max(a.ctx[r], 0), kMostLen);
+      add = min(a.add[r], kMostLen);
     }
     const int adds = max(add, 0);
-    const int pages = (int)(((long long)ctx + P - 1) >> a.page_shift);
-    const int want = (int)(((long long)ctx + adds + P - 1) >> a.page_shift);
-    const bool fits = want <= a.max_blocks;
-    const int held = min(pages, a.max_blocks);
-    const Sums own{adds, fits ? want - pages : 0, add < 0 ? held : 0};
-    Sums incl = own;
+    const uint32_t pages = ((uint32_t)ctx + P - 1) >> a.page_shift, want = ((uint32_t)ctx + adds + P - 1) >> a.page_shift;
+    const bool fits = want <= (uint32_t)a.max_blocks;
+    const int held = min((int)pages, a.max_blocks);
+    const int own[kSums] = {adds, fits ? (int)(want - pages) : 0, add < 0 ? held : 0};
+    int incl[kSums], all[kSums];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const Sums o{__shfl_up(incl.tokens, d, 64), __shfl_up(incl.need, d, 64), __shfl_up(incl.gone, d, 64)};
-      if (lane >= d) incl = incl + o;
+    for (int i = 0; i < kSums; ++i) incl[i] = wave_incl_sat(own[i]);
+    if constexpr (NW > 1) {
+      if (lane == 63)
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) sh.wave[i][wave] = incl[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kSums; ++i) {
+        const int w = wave_incl_sat(sh.wave[i][min(lane, NW - 1)]);
+        const int before = wave ? __shfl(w, wave - 1, 64) : 0;
+        incl[i] = add_sat(incl[i], add_sat(before, base[i]));
+        all[i] = add_sat(__shfl(w, NW - 1, 64), base[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSums; ++i) {
+        all[i] = add_sat(__shfl(incl[i], 63, 64), base[i]);
+        incl[i] = add_sat(incl[i], base[i]);
+      }
     }
-    if (lane == 63) sh.wave[wave] = incl;
-    __syncthreads();
-    Sums pre = base, all = base;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-      if (w < wave) pre = pre + sh.wave[w];
-      all = all + sh.wave[w];
-    }
-    incl = incl + pre;
-    const Sums excl{incl.tokens - own.tokens, incl.need - own.need, incl.gone - own.gone};
-    const bool ok = fits && (own.need == 0 || incl.need <= free0);
-    sh.tokens[tid] = clip(excl.tokens, a.T);
-    // pages taken come first in the order, so past the last one that fits the sum may stand still
-    sh.need[tid] = clip(excl.need, free0);
-    sh.gone[tid] = clip(excl.gone, a.n_pages);
+    const bool ok = fits && (own[kNeed] == 0 || incl[kNeed] <= free0);
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) sh.excl[i][tid] = incl[i] - own[i];
     sh.ctx[tid] = ctx;
     sh.held[tid] = held;
     sh.ok[tid] = ok;
-    // the chunk's pages taken: the largest sum of a request served
-    const bool takes = ok && own.need > 0;
-    long long most = takes ? incl.need : 0;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const long long o = __shfl_xor(most, d, 64);
-      most = most > o ? most : o;
-    }
-    const int no = __popcll(__ballot(r < a.R && !ok));
+    if (r < a.R && !ok) atomicAdd(&sh.refused, 1);
     __syncthreads();
-    if (lane == 0) sh.wave[wave] = Sums{no, most, 0};
-    __syncthreads();
-    long long top = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-      refused += (int)sh.wave[w].tokens;
-      top = top > sh.wave[w].need ? top : sh.wave[w].need;
-    }
-    taken = taken > top ? taken : top;
+    // pages taken: the requests served that need some come first, so up to the
+    // last sum that fits
+    if (all[kNeed] <= free0)
+      taken = all[kNeed];
+    else if (base[kNeed] <= free0)
+      taken = sh.excl[kNeed][bisect(sh.excl[kNeed], m, free0)];
     if (fill) {
       if (first && r < a.R) {
-        a.cu[r] = sh.tokens[tid];
-        a.kv_lens[r] = ok && add >= 0 ? (int)min((long long)ctx + adds, 0x7FFFFFFFLL) : 0;
+        a.cu[r] = min(incl[kTokens] - own[kTokens], a.T);
+        a.kv_lens[r] = ok && add >= 0 ? (int)min((uint32_t)ctx + adds, 0x7FFFFFFFu) : 0;
       }
-      // tokens
-      const int t1 = clip(all.tokens, a.T);
-      for (int t = clip(base.tokens, a.T) + at; t < t1; t += step) {
-        const int q = bisect(sh.tokens, m, t);
-        const int pos = sh.ctx[q] + (t - sh.tokens[q]), blk = pos >> a.page_shift;
+      for (int t = base[kTokens] + at, end = min(all[kTokens], a.T); t >= 0 && t < end; t += step) {
+        const int q = bisect(sh.excl[kTokens], m, t);
+        const int64_t pos = (int64_t)sh.ctx[q] + (t - sh.excl[kTokens][q]);
         int slot = -1;
         if (sh.ok[q]) {
-          const int page = blk < sh.held[q] ? a.table[(int64_t)(r0 + q) * a.table_stride + blk]
-                                            : a.free_pages[ring(head + (uint32_t)(sh.need[q] + blk - sh.held[q]))];
-          if ((uint32_t)page < N) slot = (page << a.page_shift) + (pos & (P - 1));
+          const int blk = (int)(pos >> a.page_shift), held_q = sh.held[q];
+          const int page = blk < held_q ? a.table[(int64_t)(r0 + q) * a.table_stride + blk]
+                                        : a.free_pages[ring(sh.excl[kNeed][q] + blk - held_q)];
+          if ((uint32_t)page < N) slot = (page << a.page_shift) + (int)(pos & (P - 1));
         }
         a.slots[t] = slot;
-        a.positions[t] = pos;
+        a.positions[t] = (int)pos;
       }
-      // pages taken, then pages given back
-      const int p1 = clip(taken, free0);
-      for (int p = clip(base.need, free0) + at; p < p1; p += step) {
-        const int q = bisect(sh.need, m, p);
-        const int blk = sh.held[q] + (p - sh.need[q]);
-        a.table[(int64_t)(r0 + q) * a.table_stride + blk] = a.free_pages[ring(head + (uint32_t)p)];
+      for (int p = base[kNeed] + at; p >= 0 && p < taken; p += step) {
+        const int q = bisect(sh.excl[kNeed], m, p);
+        a.table[(int64_t)(r0 + q) * a.table_stride + sh.held[q] + (p - sh.excl[kNeed][q])] = a.free_pages[ring(p)];
       }
-      const int g1 = clip(all.gone, a.n_pages - free0);
-      for (int p = clip(base.gone, a.n_pages) + at; p < g1; p += step) {
-        const int q = bisect(sh.gone, m, p);
-        a.free_pages[ring(head + (uint32_t)(free0 + p))] =
-            a.table[(int64_t)(r0 + q) * a.table_stride + (p - sh.gone[q])];
+      // given back: to the places past those in use
+      for (int p = base[kGone] + at, end = min(all[kGone], room); p >= 0 && p < end; p += step) {
+        const int q = bisect(sh.excl[kGone], m, p);
+        a.free_pages[ring(free0 + p)] = a.table[(int64_t)(r0 + q) * a.table_stride + (p - sh.excl[kGone][q])];
       }
     }
-    base = all;
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) base[i] = all[i];
     __syncthreads();
   }
   if (fill) {
-    const int total = clip(base.tokens, a.T);
+    const int total = min(base[kTokens], a.T);
     if (first && tid == 0) a.cu[a.R] = total;
     for (int t = total + at; t < a.T; t += step) {
       a.slots[t] = -1;
@@ -160,10 +162,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a, bool fil
     }
   }
   if (pool && first && tid == 0) {
-    const int back = clip(base.gone, a.n_pages - free0);
-    a.pool_out[0] = (int)ring(head + (uint32_t)taken);
-    a.pool_out[1] = free0 - (int)taken + back;
-    a.pool_out[2] = refused;
+    a.pool_out[0] = (int)(taken < (int)N ? ring(taken) : head);
+    a.pool_out[1] = free0 - taken + min(base[kGone], room);
+    a.pool_out[2] = a.R > 0 ? sh.refused : 0;
   }
 }
 
@@ -199,13 +200,22 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, int S) {
 }  // namespace
 
 hipError_t launch_kv_plan(const PlanArgs& a, hipStream_t s) {
+  const int work = a.R > a.T ? a.R : a.T;
+  if (work <= 64) {
+    plan_kernel<64><<<1, 64, 0, s>>>(a, true, true);
+    return hipGetLastError();
+  }
+  if (work <= 256) {
+    plan_kernel<256><<<1, 256, 0, s>>>(a, true, true);
+    return hipGetLastError();
+  }
   // pool_out may be pool_in only where no other workgroup still reads it
   const int groups = min(64, max(1, (a.T + kTokensPerGroup - 1) / kTokensPerGroup));
   const bool apart = groups > 1 && a.pool_out == a.pool_in;
-  plan_kernel<<<groups, kPlanThreads, 0, s>>>(a, true, !apart);
-  hipError_t e = hipGetLastError();
+  plan_kernel<kMaxThreads><<<groups, kMaxThreads, 0, s>>>(a, true, !apart);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !apart) return e;
-  plan_kernel<<<1, kPlanThreads, 0, s>>>(a, false, true);
+  plan_kernel<kMaxThreads><<<1, kMaxThreads, 0, s>>>(a, false, true);
   return hipGetLastError();
 }
 
