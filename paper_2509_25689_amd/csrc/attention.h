@@ -26,9 +26,10 @@ struct AttnArgs {
   int64_t table_stride;
   int32_t max_kv;  // keys that a table's row can name
   int32_t n_pages, page_shift;
+  uint32_t g_mul, g_shift;  // division by g
   int32_t HQ, HK, g, n_seqs, T, causal, window;
   float scale, c;  // c = scale * log2(e)
-  int32_t n_slots, n_wg;
+  int32_t n_slots, heads_together, n_wg;
   PagedJoin *few_join, *tile_join;
   float *few_ml, *few_part, *tile_ml, *tile_part;
 };

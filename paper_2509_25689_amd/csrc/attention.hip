@@ -2,8 +2,10 @@
 //
 // Row r of sequence s and kv head h is query token r / g, head h g + r % g (g
 // query heads share a kv head): the rows that read the same keys form tiles.
-#include "attn_core.h"
+#include <algorithm>
+
 #include "attention.h"
+#include "attn_core.h"
 
 namespace moeq {
 
@@ -49,7 +51,7 @@ __device__ __forceinline__ Span visible(const AttnArgs& a, const Seq& s, int j) 
 template <int D, int DV, bool PAGED>
 struct Keys {
   const AttnArgs& a;
-  const char *k, *v;
+  const char *k, *v;  // the head's, of a prompt's first token or of the cache
   const int32_t* table;
   int kv;
   GranuleOffsets<D / 8, true> ko;
@@ -77,34 +79,45 @@ struct Keys {
     const int b = cload(table, g >> a.page_shift);
     return (uint32_t)b < (uint32_t)a.n_pages ? b : 0;
   }
-  __device__ __forceinline__ const char* value_row(int key) const {
-    if constexpr (!PAGED) return v + (int64_t)key * a.v_row;
-    const int g = key & ~(kGranule - 1);
-    return v + page(g) * a.v_page + (int64_t)(key & ((1 << a.page_shift) - 1)) * a.v_row;
+  __device__ __forceinline__ int64_t row_at(int key, int page, int64_t page_bytes, uint32_t row_bytes) const {
+    if constexpr (PAGED) return page * page_bytes + (int64_t)(key & ((1 << a.page_shift) - 1)) * row_bytes;
+    return (int64_t)key * row_bytes;
   }
-  __device__ __forceinline__ void load(int g, int page, uint32_t k_dst, uint32_t v_dst) const {
-    const char *kp, *vp;
-    if constexpr (PAGED) {
-      const int at = g & ((1 << a.page_shift) - 1);
-      kp = k + page * a.k_page + (int64_t)at * a.k_row;
-      vp = v + page * a.v_page + (int64_t)at * a.v_row;
-    } else {
-      kp = k + (int64_t)g * a.k_row;
-      vp = v + (int64_t)g * a.v_row;
-    }
+  __device__ __forceinline__ const char* key_row(int key) const {
+    return k + row_at(key, page(key & ~(kGranule - 1)), a.k_page, a.k_row);
+  }
+  __device__ __forceinline__ const char* value_row(int key) const {
+    return v + row_at(key, page(key & ~(kGranule - 1)), a.v_page, a.v_row);
+  }
+  // granule g's keys (values).  Rows past the last key repeat it: they are
+  // masked, and what lies there may be anything.
+  __device__ __forceinline__ void load_k(int g, int page, uint32_t dst) const {
+    const char* p = k + row_at(g, page, a.k_page, a.k_row);
     if (g + kGranule <= kv) {
-      ko.load(kp, k_dst);
-      vo.load(vp, v_dst);
-    } else {  // rows past the last key repeat it (they are masked; what lies there may be anything)
-      GranuleOffsets<D / 8, true> kt;
-      GranuleOffsets<DV / 8, false> vt;
-      kt.set(a.k_row, kv - 1 - g);
-      vt.set(a.v_row, kv - 1 - g);
-      kt.load(kp, k_dst);
-      vt.load(vp, v_dst);
+      ko.load(p, dst);
+    } else {
+      GranuleOffsets<D / 8, true> t;
+      t.set(a.k_row, kv - 1 - g);
+      t.load(p, dst);
+    }
+  }
+  __device__ __forceinline__ void load_v(int g, int page, uint32_t dst) const {
+    const char* p = v + row_at(g, page, a.v_page, a.v_row);
+    if (g + kGranule <= kv) {
+      vo.load(p, dst);
+    } else {
+      GranuleOffsets<DV / 8, false> t;
+      t.set(a.v_row, kv - 1 - g);
+      t.load(p, dst);
     }
   }
 };
+
+// row / g for rows below 2^31 (g_mul = floor(2^g_shift / g) + 1, g_shift = 31 +
+// ceil(log2 g))
+__device__ __forceinline__ int div_g(const AttnArgs& a, int row) {
+  return (int)((uint64_t)(uint32_t)row * a.g_mul >> a.g_shift);
+}
 
 // The lane's row of a tile of rows that starts at row0
 struct Row {
@@ -115,10 +128,14 @@ struct Row {
 __device__ __forceinline__ Row row_of(const AttnArgs& a, const Seq& s, int row) {
   Row r;
   r.valid = row < s.n * a.g;
-  r.token = row / a.g;
+  r.token = div_g(a, row);
   r.head = row - r.token * a.g;
   r.see = r.valid ? visible(a, s, r.token) : Span{0, 0x7FFFFFFF};
   return r;
+}
+
+__device__ __forceinline__ const char* q_row(const AttnArgs& a, const Seq& s, const Row& r, int kvh) {
+  return r.valid ? a.q + (int64_t)(s.start + r.token) * a.q_row + (int64_t)(kvh * a.g + r.head) * a.q_head : nullptr;
 }
 
 template <typename T, int DV, int DB>
@@ -148,6 +165,23 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const f32x16 (&o)[D
     a.lse[(int64_t)(s.start + r.token) * a.HQ + head] = m == kLowest ? -INFINITY : m * a.scale + __logf(l);
 }
 
+// The order in which the key tiles of [lo, hi) are taken, `width` keys each, the
+// next `step` keys on: those that some row does not see whole, which take a
+// mask, before those within `all`, which every row sees.
+struct Order {
+  int lo, step, n, masked, a0, a1;  // tiles; masked ones; tiles a0 .. a1 - 1 take no mask
+  __device__ __forceinline__ Order(int lo_, int hi, int step_, int width, const Span& all) : lo(lo_), step(step_) {
+    n = max(hi - lo + step - 1, 0) / step;
+    a0 = min(n, max(all.lo - lo + step - 1, 0) / step);
+    a1 = clampi(max(min(all.hi, hi) - lo + step - width, 0) / step, a0, n);
+    masked = a0 + n - a1;
+  }
+  // first key of the i-th tile taken
+  __device__ __forceinline__ int key(int i) const {
+    return lo + (i < a0 ? i : i < masked ? i - a0 + a1 : i - masked + a0) * step;
+  }
+};
+
 // ---- tiles of 32 rows a wave ----
 // The workgroup's waves share key tiles of 64 (NW waves: each loads 64 / NW /
 // 16 granules) in two stages of LDS; each wave keeps 32 rows.
@@ -161,54 +195,111 @@ struct TileKernel {
   typedef RowBlock<T, D, DV> RB;
 
   // The tile's rows' keys [lo, hi) -> rb.  all: the keys that every row sees.
-  // Tiles within `all` take no mask; those before and after have code of their own,
-  // so that the main loop holds nothing else.
+  // begin() prepares rb, ad and r while the first tile is on its way.
+  template <typename F>
   static __device__ __forceinline__ void run(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
-                                             const Keys<D, DV, PAGED>& keys, const Row& r, int lo, int hi, Span all) {
+                                             const Keys<D, DV, PAGED>& keys, const Row& r, int lo, int hi, Span all,
+                                             F begin) {
+    static_assert(NW * kGranule == kTileKeys, "a wave loads one granule of a tile");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nt = (hi - lo + kTileKeys - 1) / kTileKeys;
-    const int a0 = min(nt, (max(all.lo - lo, 0) + kTileKeys - 1) / kTileKeys);
-    const int a1 = clampi((min(all.hi, hi) - lo) / kTileKeys, a0, nt);
-    auto load = [&](int t) {
-      const uint32_t st = base + (t & 1) * kStage;
-      const int g = keys.granule(lo + t * kTileKeys + wave * kGranule);
-      keys.load(g, keys.page(g), st + wave * (kGranule * D * 2), st + kK + wave * (kGranule * DV * 2));
+    const Order od(lo, hi, kTileKeys, kTileKeys, all);
+    const int nt = od.n;
+    auto load = [&](int i, bool k, bool v) {
+      const uint32_t st = base + (i & 1) * kStage;
+      const int g = keys.granule(od.key(i) + wave * kGranule), page = keys.page(g);
+      if (k) keys.load_k(g, page, st + wave * (kGranule * D * 2));
+      if (v) keys.load_v(g, page, st + kK + wave * (kGranule * DV * 2));
     };
-    static_assert(NW * kGranule == kTileKeys, "one granule a wave");
-    Span odd{0x7FFFFFFF, 0};  // of the blocks whose values add_nonfinite adds
-    auto tile = [&](int t, auto masked) {
-      stage_barrier();
-      if (t + 1 < nt) load(t + 1);
-      const int key = lo + t * kTileKeys, top = min(r.see.hi, keys.kv);
-      if constexpr (decltype(masked)::value)
-        if (!__any(r.valid && top > key && r.see.lo < key + kTileKeys)) return;
-      const uint32_t kt = base + (t & 1) * kStage, vt = kt + kK;
-      f32x16 s[2];
+    auto scores = [&](int i, f32x16 (&s)[2], auto between) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) s[b] = rb.scores(ad, kt + b * 32 * D * 2);
-      if constexpr (decltype(masked)::value)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) RB::mask(s[b], key + 32 * b, r.see.lo, top);
+      for (int b = 0; b < 2; ++b)
+        s[b] = rb.scores(ad, base + (i & 1) * kStage + b * 32 * D * 2, [&](int t) { between(b * RB::KS + t); });
+    };
+    auto nothing = [](int) {};
+    // Loads of tile tk's keys and tile tv's values, both without a mask (so with
+    // no granule that ends early), to the stages of tiles ik and iv (past the end
+    // the last tile's again, where no one reads them), one at a time between the
+    // steps of a product:
+    // issued together, the workgroup's waves wait for each other's (8 loads a
+    // wave 650 of a tile's 2900 cycles).  There are 2 KS steps; every second one
+    // carries a load.
+    auto spread = [&](int tk, int ik, int tv, int iv) {
+      const int gk = od.key(tk) + wave * kGranule, gv = od.key(tv) + wave * kGranule;
+      const char* kp = keys.key_row(gk);
+      const char* vp = keys.value_row(gv);
+      const uint32_t kd = base + (ik & 1) * kStage + wave * (kGranule * D * 2);
+      const uint32_t vd = base + (iv & 1) * kStage + kK + wave * (kGranule * DV * 2);
+      return [=, &keys](int step) {
+        constexpr int NK = GranuleOffsets<D / 8, true>::N, NV = GranuleOffsets<DV / 8, false>::N;
+        static_assert(2 * (NK + NV) <= 2 * RB::KS, "a step for every load");
+        if (step & 1) return;
+        const int j = step >> 1;
+        if (j < NK)
+          keys.ko.load_one(kp, kd, j);
+        else if (j < NK + NV)
+          keys.vo.load_one(vp, vd, j - NK);
+      };
+    };
+    auto finish = [&](int i, const f32x16 (&s)[2]) {
       uint32_t p[2][8];
-      rb.template softmax<2>(s, a.c, p);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint32_t v = vt + b * 32 * DV * 2;
-        const bool finite = decltype(masked)::value && RB::any_nonfinite(v);
-        if (finite) {
-          odd.lo = min(odd.lo, key + 32 * b);
-          odd.hi = key + 32 * b + 32;
-        }
-        rb.template values<decltype(masked)::value>(ad, v, p[b], finite);
-      }
+      for (int b = 0; b < 2; ++b) rb.weights(s[b], a.c, p[b]);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) rb.values(ad, base + (i & 1) * kStage + kK + b * 32 * DV * 2, p[b]);
     };
-    if (nt > 0) load(0);
-    int t = 0;
-    for (; t < a0; ++t) tile(t, std::true_type());
-    for (; t < a1; ++t) tile(t, std::false_type());
-    for (; t < nt; ++t) tile(t, std::true_type());
-    if (odd.lo < odd.hi)
-      rb.add_nonfinite(odd.lo, min(odd.hi, hi), r.see.lo, r.see.hi, [&](int key) { return keys.value_row(key); });
+    if (nt > 0) load(0, true, true);
+    begin();
+    for (int i = 0; i < od.masked; ++i) {
+      stage_barrier();
+      if (i + 1 < nt) load(i + 1, true, true);
+      const int key = od.key(i), top = min(r.see.hi, keys.kv);
+      if (!__any(r.valid && top > key && r.see.lo < key + kTileKeys)) continue;
+      f32x16 s[2];
+      scores(i, s, nothing);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) RB::mask(s[b], key + 32 * b, r.see.lo, top);
+      rb.rescale(RB::template largest<2>(s), a.c);
+      finish(i, s);
+    }
+    if (od.masked > 0 && !rb.finite())
+      rb.redo(a.c, r.see.lo, min(r.see.hi, keys.kv), od.masked, kTileKeys, hi, [&](int i) { return od.key(i); },
+              [&](int key) { return keys.key_row(key); }, [&](int key) { return keys.value_row(key); });
+    if constexpr (D > 128) {
+      // (the scores of two tiles do not fit the registers beside 192-wide queries)
+      for (int i = od.masked; i < nt; ++i) {
+        stage_barrier();
+        f32x16 s[2];
+        scores(i, s, spread(min(i + 1, nt - 1), i + 1, min(i + 1, nt - 1), i + 1));
+        rb.rescale(RB::template largest<2>(s), a.c);
+        finish(i, s);
+      }
+    } else if (od.masked < nt) {
+      // The other tiles, one ahead: the scores of the next tile are formed on the
+      // matrix cores while the vector units take this one's exponentials.
+      auto step = [&](int i, const f32x16 (&s)[2], f32x16 (&next)[2]) {
+        rb.rescale(RB::template largest<2>(s), a.c);
+        stage_barrier();  // the next tile's keys and this one's values are there
+        scores(i + 1, next, spread(min(i + 2, nt - 1), i + 2, i + 1, i + 1));
+        finish(i, s);
+      };
+      f32x16 s0[2], s1[2];
+      int i = od.masked;
+      stage_barrier();
+      if (i + 1 < nt) load(i + 1, true, false);
+      scores(i, s0, nothing);
+      for (; i + 2 < nt; i += 2) {
+        step(i, s0, s1);
+        step(i + 1, s1, s0);
+      }
+      if (i + 1 < nt) {
+        step(i++, s0, s1);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s0[b] = s1[b];
+      }
+      rb.rescale(RB::template largest<2>(s0), a.c);
+      stage_barrier();
+      finish(i, s0);
+    }
     stage_barrier();
   }
 };
@@ -222,14 +313,15 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
   extern __shared__ char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Workgroup b runs on XCD b % 8.  With a multiple of 8 kv heads an XCD takes
-  // whole heads, one after the other, so that its L2 holds their keys; late
-  // tiles, which see the most keys, come first.
+  // whole heads, a.heads_together of them at a time, so that its L2 holds their
+  // keys; late tiles, which see the most keys, come first.
   const int b = blockIdx.x;
   int kvh, slot;
   if (a.HK % 8 == 0) {
-    const int j = b >> 3;
-    kvh = (b & 7) + 8 * (j / a.n_slots);
-    slot = a.n_slots - 1 - j % a.n_slots;
+    const int j = b >> 3, per = a.heads_together, group = j / (a.n_slots * per), in = j - group * (a.n_slots * per);
+    const int heads = min(per, a.HK / 8 - group * per);
+    kvh = (b & 7) + 8 * (group * per + in % heads);
+    slot = a.n_slots - 1 - in / heads;
   } else {
     kvh = b % a.HK;
     slot = a.n_slots - 1 - b / a.HK;
@@ -247,19 +339,20 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
   const Seq s = prompt_seq(a, seq);
   const int row0 = (slot - __builtin_amdgcn_readfirstlane(first_slot(seq))) * TK::BM;
   if (row0 < 0 || row0 >= s.n * a.g) return;
-  const Row r = row_of(a, s, row0 + wave * 32 + (lane & 31));
   const int last = min(row0 + TK::BM, s.n * a.g) - 1;
-  const Span v0 = visible(a, s, row0 / a.g), v1 = visible(a, s, last / a.g);
+  const Span v0 = visible(a, s, div_g(a, row0)), v1 = visible(a, s, div_g(a, last));
   const int lo = v0.lo & ~(kGranule - 1), hi = min(v1.hi, s.kv);
-
-  typename TK::RB rb;
-  typename TK::RB::Addr ad;
-  ad.set();
-  rb.clear();
-  rb.load_q(r.valid ? a.q + (int64_t)(s.start + r.token) * a.q_row + (int64_t)(kvh * a.g + r.head) * a.q_head : nullptr);
   Keys<D, DV, false> keys(a);
   keys.seq(s, seq, kvh);
-  TK::run(a, lds_addr(smem), rb, ad, keys, r, lo, hi, Span{v1.lo, min(v0.hi, s.kv)});
+  Row r;
+  typename TK::RB rb;
+  typename TK::RB::Addr ad;
+  TK::run(a, lds_addr(smem), rb, ad, keys, r, lo, hi, Span{v1.lo, min(v0.hi, s.kv)}, [&] {
+    r = row_of(a, s, row0 + wave * 32 + (lane & 31));
+    rb.load_q(q_row(a, s, r, kvh));
+    ad.set();
+    rb.clear();
+  });
   store_out<T, DV>(a, rb.o, rb.m, sum_halves(rb.l), s, r, kvh);
 }
 
@@ -281,8 +374,8 @@ struct Work {
   }
   static __device__ __forceinline__ Span span(const AttnArgs& a, const Seq& s, int qt) {
     const int rows = s.n * a.g, row0 = qt * BM, last = min(row0 + BM, rows) - 1;
-    const int hi = min(visible(a, s, last / a.g).hi, s.kv);
-    return Span{min(visible(a, s, row0 / a.g).lo, hi) & ~(kGranule - 1), hi};
+    const int hi = min(visible(a, s, div_g(a, last)).hi, s.kv);
+    return Span{min(visible(a, s, div_g(a, row0)).lo, hi) & ~(kGranule - 1), hi};
   }
   // at least 1: rows that see nothing are written too
   static __device__ __forceinline__ int key_tiles(const Span& p) { return max(1, (p.hi - p.lo + BN - 1) / BN); }
@@ -438,15 +531,16 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
   Keys<D, DV, true> keys(a);
   each_piece<W, 64 * NW>(a, a.tile_join, [&](int kvh, int r, const Seq& s, int qt, const Span& sp, int t0, int n, bool whole, int slot) {
     const int in = wave * 32 + (lane & 31);
-    const Row row = row_of(a, s, qt * TK::BM + in);
-    rb.clear();
-    rb.load_q(row.valid ? a.q + (int64_t)(s.start + row.token) * a.q_row + (int64_t)(kvh * a.g + row.head) * a.q_head
-                        : nullptr);
     keys.seq(s, r, kvh);
     const int lo = sp.lo + t0 * kTileKeys;
     const int row0 = qt * TK::BM, last = min(row0 + TK::BM, s.n * a.g) - 1;
+    Row row;
     TK::run(a, lds_addr(smem), rb, ad, keys, row, lo, min(sp.hi, lo + n * kTileKeys),
-            Span{visible(a, s, last / a.g).lo, min(visible(a, s, row0 / a.g).hi, s.kv)});
+            Span{visible(a, s, div_g(a, last)).lo, min(visible(a, s, div_g(a, row0)).hi, s.kv)}, [&] {
+              row = row_of(a, s, row0 + in);
+              rb.load_q(q_row(a, s, row, kvh));
+              rb.clear();
+            });
     const float l = sum_halves(rb.l);
     if (whole) {
       store_out<T, DV>(a, rb.o, rb.m, l, s, row, kvh);
@@ -495,53 +589,44 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
   ad.set();
   Keys<D, DV, true> keys(a);
   each_piece<W, 64 * NW>(a, a.few_join, [&](int kvh, int r, const Seq& s, int, const Span& sp, int t0, int n, bool whole, int slot) {
-    const Row row = row_of(a, s, lane & 31);
-    rb.clear();
-    rb.load_q(row.valid ? a.q + (int64_t)(s.start + row.token) * a.q_row + (int64_t)(kvh * a.g + row.head) * a.q_head
-                        : nullptr);
     keys.seq(s, r, kvh);
-    const int first = sp.lo + t0 * FK::BN + wave * 32;
-    // this wave's tiles: those with a key below sp.hi
-    const int mine_n = min(n, max(0, (sp.hi - first + FK::BN - 1) / FK::BN));
-    auto load = [&](int t) {
-      const uint32_t st = mine + (t & 1) * FK::kStage;
+    const Order od(sp.lo + t0 * FK::BN + wave * 32, min(sp.hi, sp.lo + (t0 + n) * FK::BN), FK::BN, 32,
+                   Span{visible(a, s, s.n - 1).lo, min(visible(a, s, 0).hi, s.kv)});
+    auto load = [&](int i) {
+      const uint32_t st = mine + (i & 1) * FK::kStage;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int g = keys.granule(first + t * FK::BN + i * kGranule);
-        keys.load(g, keys.page(g), st + i * (kGranule * D * 2), st + FK::kK + i * (kGranule * DV * 2));
+      for (int j = 0; j < 2; ++j) {
+        const int g = keys.granule(od.key(i) + j * kGranule), page = keys.page(g);
+        keys.load_k(g, page, st + j * (kGranule * D * 2));
+        keys.load_v(g, page, st + FK::kK + j * (kGranule * DV * 2));
       }
     };
-    Span odd{0x7FFFFFFF, 0};
-    if (mine_n > 0) load(0);
-    if (mine_n > 1) load(1);
-    for (int t = 0; t < mine_n; ++t) {
-      if (t + 1 < mine_n)
+    if (od.n > 0) load(0);
+    if (od.n > 1) load(1);
+    const Row row = row_of(a, s, lane & 31);
+    rb.load_q(q_row(a, s, row, kvh));
+    rb.clear();
+    const int top = min(row.see.hi, s.kv);
+    auto tile = [&](int i, bool masked) {
+      if (i + 1 < od.n)
         wait_loads<FK::kLoads>();
       else
         wait_loads<0>();
-      const int key = first + t * FK::BN;
-      const uint32_t kt = mine + (t & 1) * FK::kStage;
-      f32x16 sc[1];
-      sc[0] = rb.scores(ad, kt);
-      const int top = min(row.see.hi, s.kv);
-      const bool hides = __any(row.see.lo > key || top < key + 32);
-      if (hides) RB::mask(sc[0], key, row.see.lo, top);
-      uint32_t p[1][8];
-      rb.template softmax<1>(sc, a.c, p);
-      const bool finite = hides && RB::any_nonfinite(kt + FK::kK);
-      if (finite) {
-        odd.lo = min(odd.lo, key);
-        odd.hi = key + 32;
-      }
-      rb.template values<true>(ad, kt + FK::kK, p[0], finite);
+      const uint32_t kt = mine + (i & 1) * FK::kStage;
+      f32x16 sc[1] = {rb.scores(ad, kt, [](int) {})};
+      if (masked) RB::mask(sc[0], od.key(i), row.see.lo, top);
+      rb.rescale(RB::template largest<1>(sc), a.c);
+      uint32_t p[8];
+      rb.weights(sc[0], a.c, p);
+      rb.values(ad, kt + FK::kK, p);
       wait_lds();
-      if (t + 2 < mine_n) load(t + 2);
-    }
-    if (odd.lo < odd.hi) {
-      // this wave's blocks only: 32 keys every BN
-      for (int key = odd.lo; key < min(odd.hi, s.kv); key += FK::BN)
-        rb.add_nonfinite(key, min(key + 32, s.kv), row.see.lo, row.see.hi, [&](int k) { return keys.value_row(k); });
-    }
+      if (i + 2 < od.n) load(i + 2);
+    };
+    for (int i = 0; i < od.masked; ++i) tile(i, true);
+    if (od.masked > 0 && !rb.finite())
+      rb.redo(a.c, row.see.lo, top, od.masked, 32, s.kv, [&](int i) { return od.key(i); },
+              [&](int key) { return keys.key_row(key); }, [&](int key) { return keys.value_row(key); });
+    for (int i = od.masked; i < od.n; ++i) tile(i, false);
     // join the waves
     const float l = sum_halves(rb.l);
     if (h == 0) {
@@ -585,7 +670,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
       const float m = ml[0][rr][0], lr = ml[0][rr][1];
       if (whole) {
         const float inv = lr > 0.0f || !(lr == lr) ? 1.0f / lr : 0.0f;
-        const int token = rr / a.g, head = kvh * a.g + rr - token * a.g;
+        const int token = div_g(a, rr), head = kvh * a.g + rr - token * a.g;
         *(u32x4*)(a.out + (int64_t)(s.start + token) * a.o_row + (int64_t)head * a.o_head + col * 2) =
             u32x4{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv), T::pack(y[0] * inv, y[1] * inv),
                   T::pack(y[2] * inv, y[3] * inv)};
@@ -632,7 +717,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, const Paged
       for (int j = 0; j < NC; ++j) o[j] += f * part[at * DV + lane * NC + j];
     }
     const float inv = L > 0.0f || !(L == L) ? 1.0f / L : 0.0f;
-    const int token = (row0 + row) / a.g, head = rec.kvh * a.g + (row0 + row) % a.g;
+    const int token = div_g(a, row0 + row), head = rec.kvh * a.g + row0 + row - token * a.g;
     char* out = a.out + (int64_t)(rec.start + token) * a.o_row + (int64_t)head * a.o_head;
     const uint32_t u = T::pack(o[0] * inv, o[NC - 1] * inv);
     if constexpr (NC == 2)
@@ -671,6 +756,12 @@ hipError_t launch_attn_prompt(AttnArgs a, int dtype, int D, hipStream_t s) {
     if (e != hipSuccess) return e;
     const long long slots = (long long)a.T * a.g / TK::BM + a.n_seqs;
     a.n_slots = (int)slots;
+    // Heads in turn leave an XCD's 64 places (two a compute unit) uneven at the
+    // end: the last ones' longest tile starts when the others are nearly done.
+    // So many at once that they give each place at least that tile's work (of
+    // slots (slots + 1) / 2 a head): 128 heads of 2048 tokens in 219 us, one
+    // after the other in 238, all 16 of an XCD together (its L2 misses) in 225.
+    a.heads_together = (int)std::max<long long>(1, std::min<long long>(a.HK / 8, (2 * 64 + slots) / (slots + 1)));
     kernel<<<(unsigned)(slots * a.HK), 64 * NW, TK::lds, s>>>(a);
     return hipGetLastError();
   });

@@ -27,6 +27,13 @@ bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s < ((int64_t)1 << 40
 // rows whose 16 neighbours' offsets the kernels keep in 32 bits
 bool row_stride_ok(int64_t s) { return stride_ok(s) && s < ((int64_t)1 << 26); }
 
+// the smallest s with 2^s >= p
+int log2_of(int p) {
+  int s = 0;
+  while ((1 << s) < p) ++s;
+  return s;
+}
+
 constexpr int kMaxHeads = 4096;
 constexpr int kMaxGroup = 256;
 constexpr int kMaxRows = 1 << 24;  // tokens of a call
@@ -69,12 +76,6 @@ moeq_status check_rows(const moeq_rows* r, const char* name, bool neighbours) {
   return MOEQ_OK;
 }
 
-int log2_of(int p) {
-  int s = 0;
-  while ((1 << s) < p) ++s;
-  return s;
-}
-
 moeq_status check_pages(int32_t page_size, int32_t n_pages) {
   if (page_size < 16 || page_size > 4096 || (page_size & (page_size - 1)))
     return fail(MOEQ_ERR_INVALID_ARG, "page_size %d must be a power of two, 16 .. 4096", page_size);
@@ -99,6 +100,8 @@ void set_heads(AttnArgs& g, const moeq_attn* a) {
   g.HQ = a->n_heads;
   g.HK = a->n_kv_heads;
   g.g = a->n_heads / a->n_kv_heads;
+  g.g_shift = 31 + log2_of(g.g);
+  g.g_mul = (uint32_t)(((uint64_t)1 << g.g_shift) / g.g + 1);
   g.causal = a->causal;
   g.window = a->window;
   g.scale = a->scale;

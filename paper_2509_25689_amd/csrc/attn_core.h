@@ -29,10 +29,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 
-// low, high: a dword's two values; kExponent: both exponent fields, and one of
-// their lowest bits each (a field of ones carries into the sign)
+// low, high: a dword's two values
 struct Bf16 {
-  static constexpr uint32_t kExponent = 0x7F807F80u, kExponentStep = 0x00800080u;
   static __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
   static __device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
   static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
@@ -46,7 +44,6 @@ struct Bf16 {
 };
 
 struct F16 {
-  static constexpr uint32_t kExponent = 0x7C007C00u, kExponentStep = 0x04000400u;
   static __device__ __forceinline__ float low(uint32_t v) { return (float)__builtin_bit_cast(f16x2, v)[0]; }
   static __device__ __forceinline__ float high(uint32_t v) { return (float)__builtin_bit_cast(f16x2, v)[1]; }
   static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
@@ -115,9 +112,12 @@ struct GranuleOffsets {
       off[i] = (uint32_t)min(r, last_row) * row_bytes + (uint32_t)(IsK ? k_swz<C>(r, c) : v_swz<C>(r, c)) * 16u;
     }
   }
+  __device__ __forceinline__ void load_one(const char* base, uint32_t dst, int i) const {
+    load_lds(base, off[i], dst + 1024u * i);
+  }
   __device__ __forceinline__ void load(const char* base, uint32_t dst) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) load_lds(base, off[i], dst + 1024u * i);
+    for (int i = 0; i < N; ++i) load_one(base, dst, i);
   }
 };
 
@@ -189,13 +189,17 @@ struct RowBlock {
     }
   };
 
-  // scores of the 32 keys at LDS address kt
-  __device__ __forceinline__ f32x16 scores(const Addr& a, uint32_t kt) const {
+  // scores of the 32 keys at LDS address kt; between(t) after step t
+  template <typename F>
+  __device__ __forceinline__ f32x16 scores(const Addr& a, uint32_t kt, F between) const {
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-    for (int t = 0; t < KS; ++t) s = T::mma(lds_read16(kt + a.k[t]), q[t], s);
+    for (int t = 0; t < KS; ++t) {
+      s = T::mma(lds_read16(kt + a.k[t]), q[t], s);
+      between(t);
+    }
     return s;
   }
 
@@ -216,12 +220,16 @@ struct RowBlock {
   // values before that rounding.
   static constexpr float kSlack = 8.0f;
   template <int NB>
-  __device__ __forceinline__ void softmax(f32x16 (&s)[NB], float c, uint32_t (&p)[NB][8]) {
+  static __device__ __forceinline__ float largest(const f32x16 (&s)[NB]) {
     float t = s[0][0];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) t = fmaxf(t, s[b][i]);
+    return t;
+  }
+  // t: the lane's largest new score
+  __device__ __forceinline__ void rescale(float t, float c) {
     t = max_halves(t);
     if (__any(fmaf(t, c, neg_mc) > kSlack || (m == kLowest && t > kLowest))) {
       const float mn = fmaxf(m, t);
@@ -235,21 +243,18 @@ struct RowBlock {
       m = mn;
       neg_mc = nmc;
     }
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float x = exp2_fast(fmaf(s[b][i], c, neg_mc)), y = exp2_fast(fmaf(s[b][i + 1], c, neg_mc));
-        l += x;
-        l += y;
-        p[b][i / 2] = T::pack(x, y);
-      }
   }
-
-  // o += P V for the 32 keys at LDS address vt.  With MASKED and `finite`,
-  // infinities and NaN of V count as zeros.
-  template <bool MASKED = false>
-  __device__ __forceinline__ void values(const Addr& a, uint32_t vt, const uint32_t (&p)[8], bool finite = false) {
+  __device__ __forceinline__ void weights(const f32x16& s, float c, uint32_t (&p)[8]) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float x = exp2_fast(fmaf(s[i], c, neg_mc)), y = exp2_fast(fmaf(s[i + 1], c, neg_mc));
+      l += x;
+      l += y;
+      p[i / 2] = T::pack(x, y);
+    }
+  }
+  // o += P V for the 32 keys at LDS address vt
+  __device__ __forceinline__ void values(const Addr& a, uint32_t vt, const uint32_t (&p)[8]) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const u32x4 pb = {p[4 * t], p[4 * t + 1], p[4 * t + 2], p[4 * t + 3]};
@@ -257,58 +262,67 @@ struct RowBlock {
       for (int b = 0; b < DB; ++b) {
         const u32x2 x = lds_read_tr(vt + a.v[b] + (16 * t) * VC * 16);
         const u32x2 y = lds_read_tr(vt + a.v[b] + (16 * t + 8) * VC * 16);
-        u32x4 v = {x.x, x.y, y.x, y.y};
-        if (MASKED && finite)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] &= ~nonfinite(v[j]);
-        o[b] = T::mma(v, pb, o[b]);
+        o[b] = T::mma(u32x4{x.x, x.y, y.x, y.y}, pb, o[b]);
       }
     }
   }
 
-  // A key that a row does not see has weight 0 there, and 0 times an infinity
-  // or NaN must not reach the row.  Where some row of a block does not see some
-  // key and the block's values are not all finite (any_nonfinite), the product
-  // takes only the finite ones, and those rows that do see the others get them
-  // at the end (add_nonfinite): an infinity of any positive weight is one.
-  // all ones in the halves of v that hold an infinity or NaN
-  static __device__ __forceinline__ uint32_t nonfinite(uint32_t v) {
-    const uint32_t m = ((v & T::kExponent) + T::kExponentStep) & 0x80008000u;
-    return (m - (m >> 15)) | m;
-  }
-  // whether a value of the 32 keys at vt is infinite or NaN
-  static __device__ __forceinline__ bool any_nonfinite(uint32_t vt) {
-    const int lane = threadIdx.x & 63;
-    uint32_t f = 0;
-#pragma unroll 1
-    for (int i = 0; i < DV / 16; ++i) {
-      const u32x4 x = lds_read16(vt + (uint32_t)(i * 64 + lane) * 16u);
+  // A key that a row does not see has weight 0, but 0 times an infinity or NaN
+  // among its values is NaN.  So the key tiles that need a mask come first, and
+  // where o is not finite after them it is formed anew, key by key on the vector
+  // units, from the keys each row sees among the `width` keys of each of `tiles`
+  // tiles, tile_key(i) the first; key_row(key) and value_row(key) point at a
+  // key's rows (global), keys from `end` on do not exist.  m and l hold already.
+  __device__ __forceinline__ bool finite() const {
+    // (largest magnitude; a NaN makes the sum NaN)
+    float t = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f |= nonfinite(x[j]);
-    }
-    return __any(f != 0);
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t = fmaf(o[b][i], 0.0f, t);
+    return !__any(t != t);
   }
-
-  // keys first .. end - 1, whose value rows value_row(key) points at (global);
-  // the lane's row sees [lo, hi)
-  template <typename F>
-  __device__ __forceinline__ void add_nonfinite(int first, int end, int lo, int hi, F value_row) {
+  template <typename FT, typename FK, typename FV>
+  __device__ __forceinline__ void redo(float c, int lo, int hi, int tiles, int width, int end, FT tile_key, FK key_row,
+                                       FV value_row) {
     const int h = (threadIdx.x >> 5) & 1;
 #pragma unroll
-    for (int c = 0; c < 4 * DB; ++c) {  // columns 8 c + 4 h .. + 3
-      float e[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 1
-      for (int key = first; key < end; ++key) {
-        const u32x2 v = *gptr((const u32x2*)(value_row(key) + 16 * c + 8 * h));
-        const bool seen = key >= lo && key < hi;
-        const uint32_t f0 = seen ? nonfinite(v.x) : 0u, f1 = seen ? nonfinite(v.y) : 0u;
-        e[0] += f0 & 0xFFFFu ? T::low(v.x) : 0.0f;
-        e[1] += f0 >> 16 ? T::high(v.x) : 0.0f;
-        e[2] += f1 & 0xFFFFu ? T::low(v.y) : 0.0f;
-        e[3] += f1 >> 16 ? T::high(v.y) : 0.0f;
-      }
+    for (int b = 0; b < DB; ++b) {
+      float e[16];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[c / 4][4 * (c % 4) + j] += e[j];
+      for (int i = 0; i < 16; ++i) e[i] = 0.0f;
+#pragma unroll 1
+      for (int tile = 0; tile < tiles; ++tile)
+#pragma unroll 1
+        for (int key = tile_key(tile), stop = min(key + width, end); key < stop; ++key) {
+          const char* kr = key_row(key) + 16 * h;
+          float s = 0.0f;
+#pragma unroll
+          for (int t = 0; t < KS; ++t) {
+            u32x4 y = q[t];
+            asm volatile("" : "+v"(y));  // (or the unpacked queries stay in registers throughout)
+            const u32x4 x = *gptr((const u32x4*)(kr + 32 * t));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              s = fmaf(T::low(x[j]), T::low(y[j]), s);
+              s = fmaf(T::high(x[j]), T::high(y[j]), s);
+            }
+          }
+          s = sum_halves(s);
+          const float w = T::low(T::pack(exp2_fast(fmaf(s, c, neg_mc)), 0.0f));
+          const bool seen = key >= lo && key < hi;
+          const char* vr = value_row(key) + 64 * b + 8 * h;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const u32x2 v = *gptr((const u32x2*)(vr + 16 * g));
+            e[4 * g + 0] += seen ? w * T::low(v.x) : 0.0f;
+            e[4 * g + 1] += seen ? w * T::high(v.x) : 0.0f;
+            e[4 * g + 2] += seen ? w * T::low(v.y) : 0.0f;
+            e[4 * g + 3] += seen ? w * T::high(v.y) : 0.0f;
+          }
+        }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][i] = e[i];
     }
   }
 };
