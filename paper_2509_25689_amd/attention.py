@@ -13,6 +13,8 @@ of a head together ("hnd") or all heads of a place ("nhd").  Work goes to
 Tensors made by an earlier call on another stream are the caller's to order, as
 everywhere in torch; those made here are kept for ``stream``.
 """
+import functools
+
 import torch
 
 from . import moeq
@@ -67,14 +69,19 @@ def _rows(name, t, dtype, shape, device):
 
 
 def _cache(k, v, dtype, device):
-    for name, t, shape in (("k_cache", k, (None,) * 4), ("v_cache", v, None)):
-        shape = shape or (*k.shape[:3], None)
-        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.dim() == 4
-                and t.shape[:3] == k.shape[:3] and t.stride(3) == 1):
-            _refuse(name, t, dtype, shape, device)
-    n, places, heads, _ = k.shape
-    kp, ks, kh, _ = k.stride()
-    vp, vs, vh, _ = v.stride()
+    """A moeq_kv_cache of k and v."""
+    if not (isinstance(k, torch.Tensor) and k.dtype is dtype and k.get_device() == device and k.dim() == 4):
+        _refuse("k_cache", k, dtype, (None,) * 4, device)
+    n, places, heads, dim = k.shape
+    if not (isinstance(v, torch.Tensor) and v.dtype is dtype and v.get_device() == device and v.dim() == 4
+            and v.shape[:3] == (n, places, heads)):
+        _refuse("v_cache", v, dtype, (n, places, heads, None), device)
+    kp, ks, kh, k1 = k.stride()
+    vp, vs, vh, v1 = v.stride()
+    if k1 != 1:
+        _refuse("k_cache", k, dtype, (None,) * 4, device)
+    if v1 != 1:
+        _refuse("v_cache", v, dtype, (None,) * 4, device)
     if n == 1:
         kp = vp = 0
     if heads == 1:
@@ -82,12 +89,19 @@ def _cache(k, v, dtype, device):
     return moeq.moeq_kv_cache(k.data_ptr(), v.data_ptr(), n, places, kp, ks, kh, vp, vs, vh)
 
 
+@functools.lru_cache(maxsize=64)
 def _attn(heads, kv_heads, dim, value_dim, dtype, causal=True, window=0, scale=None):
+    """A moeq_attn (read only by the calls)."""
     code = _DTYPES.get(dtype)
     if code is None:
         raise ValueError(f"dtype must be bfloat16 or float16, got {dtype}")
     return moeq.moeq_attn(heads, kv_heads, dim, value_dim, code, 1 if causal else 0, window,
                           dim ** -0.5 if scale is None else scale)
+
+
+@functools.lru_cache(maxsize=64)
+def _workspace_bytes(heads, kv_heads, dim, value_dim, dtype, max_new):
+    return moeq.moeq_attn_paged_workspace(_attn(heads, kv_heads, dim, value_dim, dtype), max_new)
 
 
 def _on(name, t, dims, stream):
@@ -214,7 +228,7 @@ def paged(q, k_cache, v_cache, cu_q, kv_lens, block_table, *, max_new, causal=Tr
     args = (_rows("q", q, dt, (T, heads, dim), dev), c, _ints("cu_q", cu_q, R + 1, dev), _ints("kv_lens", kv_lens, R, dev),
             table, stride, blocks, R, T, max_new)
     if workspace is None:
-        workspace = _new(q, moeq.moeq_attn_paged_workspace(a, max_new), torch.uint8, other)
+        workspace = _new(q, _workspace_bytes(heads, kv_heads, dim, value_dim, dt, max_new), torch.uint8, other)
     elif not (workspace.dtype is torch.uint8 and workspace.get_device() == dev and workspace.dim() == 1
               and workspace.is_contiguous()):
         _refuse("workspace", workspace, torch.uint8, (None,), dev)
@@ -228,4 +242,4 @@ def paged(q, k_cache, v_cache, cu_q, kv_lens, block_table, *, max_new, causal=Tr
 
 def paged_workspace(heads, kv_heads, dim, value_dim, *, max_new, dtype=torch.bfloat16):
     """Bytes of paged's workspace, whatever the lengths."""
-    return moeq.moeq_attn_paged_workspace(_attn(heads, kv_heads, dim, value_dim, dtype), max_new)
+    return _workspace_bytes(heads, kv_heads, dim, value_dim, dtype, max_new)

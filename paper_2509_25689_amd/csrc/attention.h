@@ -29,7 +29,8 @@ struct AttnArgs {
   uint32_t g_mul, g_shift;  // division by g
   int32_t HQ, HK, g, n_seqs, T, causal, window;
   float scale, c;  // c = scale * log2(e)
-  int32_t n_slots, heads_together, n_wg;
+  int32_t whole;  // segments are not cut: the run that holds a segment's first unit takes it
+  int32_t n_slots, heads_together;
   PagedJoin *few_join, *tile_join;
   float *few_ml, *few_part, *tile_ml, *tile_part;
 };

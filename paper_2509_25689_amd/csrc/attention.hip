@@ -6,6 +6,7 @@
 
 #include "attention.h"
 #include "attn_core.h"
+#include "route_wave.h"
 
 namespace moeq {
 
@@ -48,14 +49,15 @@ __device__ __forceinline__ Span visible(const AttnArgs& a, const Seq& s, int j) 
 }
 
 // Where a sequence's keys and values lie, and the loads of 16 of them into LDS.
-template <int D, int DV, bool PAGED>
+// ONCE: no one else reads them.
+template <int D, int DV, bool PAGED, bool ONCE>
 struct Keys {
   const AttnArgs& a;
   const char *k, *v;  // the head's, of a prompt's first token or of the cache
   const int32_t* table;
   int kv;
-  GranuleOffsets<D / 8, true> ko;
-  GranuleOffsets<DV / 8, false> vo;
+  GranuleOffsets<D / 8, true, ONCE> ko;
+  GranuleOffsets<DV / 8, false, ONCE> vo;
   __device__ __forceinline__ explicit Keys(const AttnArgs& args) : a(args) {
     ko.set(a.k_row, kGranule - 1);
     vo.set(a.v_row, kGranule - 1);
@@ -96,7 +98,7 @@ struct Keys {
     if (g + kGranule <= kv) {
       ko.load(p, dst);
     } else {
-      GranuleOffsets<D / 8, true> t;
+      GranuleOffsets<D / 8, true, ONCE> t;
       t.set(a.k_row, kv - 1 - g);
       t.load(p, dst);
     }
@@ -106,7 +108,7 @@ struct Keys {
     if (g + kGranule <= kv) {
       vo.load(p, dst);
     } else {
-      GranuleOffsets<DV / 8, false> t;
+      GranuleOffsets<DV / 8, false, ONCE> t;
       t.set(a.v_row, kv - 1 - g);
       t.load(p, dst);
     }
@@ -198,7 +200,7 @@ struct TileKernel {
   // begin() prepares rb, ad and r while the first tile is on its way.
   template <typename F>
   static __device__ __forceinline__ void run(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
-                                             const Keys<D, DV, PAGED>& keys, const Row& r, int lo, int hi, Span all,
+                                             const Keys<D, DV, PAGED, false>& keys, const Row& r, int lo, int hi, Span all,
                                              F begin) {
     static_assert(NW * kGranule == kTileKeys, "a wave loads one granule of a tile");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -216,21 +218,23 @@ struct TileKernel {
         s[b] = rb.scores(ad, base + (i & 1) * kStage + b * 32 * D * 2, [&](int t) { between(b * RB::KS + t); });
     };
     auto nothing = [](int) {};
-    // Loads of tile tk's keys and tile tv's values, both without a mask (so with
-    // no granule that ends early), to the stages of tiles ik and iv (past the end
-    // the last tile's again, where no one reads them), one at a time between the
-    // steps of a product:
+    // the page of this wave's granule of the i-th tile (at most the last)
+    auto page_of = [&](int i) { return keys.page(od.key(min(i, nt - 1)) + wave * kGranule); };
+    // Loads of tile tk's keys and tile tv's values, in pages pk and pv, both
+    // without a mask (so with no granule that ends early), to the stages of tiles
+    // ik and iv (past the end the last tile's again, where no one reads them), one
+    // at a time between the steps of a product:
     // issued together, the workgroup's waves wait for each other's (8 loads a
     // wave 650 of a tile's 2900 cycles).  There are 2 KS steps; every second one
     // carries a load.
-    auto spread = [&](int tk, int ik, int tv, int iv) {
+    auto spread = [&](int tk, int ik, int pk, int tv, int iv, int pv) {
       const int gk = od.key(tk) + wave * kGranule, gv = od.key(tv) + wave * kGranule;
-      const char* kp = keys.key_row(gk);
-      const char* vp = keys.value_row(gv);
+      const char* kp = keys.k + keys.row_at(gk, pk, a.k_page, a.k_row);
+      const char* vp = keys.v + keys.row_at(gv, pv, a.v_page, a.v_row);
       const uint32_t kd = base + (ik & 1) * kStage + wave * (kGranule * D * 2);
       const uint32_t vd = base + (iv & 1) * kStage + kK + wave * (kGranule * DV * 2);
       return [=, &keys](int step) {
-        constexpr int NK = GranuleOffsets<D / 8, true>::N, NV = GranuleOffsets<DV / 8, false>::N;
+        constexpr int NK = GranuleOffsets<D / 8, true, false>::N, NV = GranuleOffsets<DV / 8, false, false>::N;
         static_assert(2 * (NK + NV) <= 2 * RB::KS, "a step for every load");
         if (step & 1) return;
         const int j = step >> 1;
@@ -266,24 +270,29 @@ struct TileKernel {
               [&](int key) { return keys.key_row(key); }, [&](int key) { return keys.value_row(key); });
     if constexpr (D > 128) {
       // (the scores of two tiles do not fit the registers beside 192-wide queries)
+      int page1 = od.masked < nt ? page_of(od.masked + 1) : 0;
       for (int i = od.masked; i < nt; ++i) {
         stage_barrier();
         f32x16 s[2];
-        scores(i, s, spread(min(i + 1, nt - 1), i + 1, min(i + 1, nt - 1), i + 1));
+        const int t1 = min(i + 1, nt - 1);
+        scores(i, s, spread(t1, i + 1, page1, t1, i + 1, page1));
+        page1 = page_of(i + 2);
         rb.rescale(RB::template largest<2>(s), a.c);
         finish(i, s);
       }
     } else if (od.masked < nt) {
       // The other tiles, one ahead: the scores of the next tile are formed on the
       // matrix cores while the vector units take this one's exponentials.
+      int i = od.masked, page1 = page_of(i + 1), page2 = page_of(i + 2);  // of tiles i + 1, i + 2
       auto step = [&](int i, const f32x16 (&s)[2], f32x16 (&next)[2]) {
         rb.rescale(RB::template largest<2>(s), a.c);
         stage_barrier();  // the next tile's keys and this one's values are there
-        scores(i + 1, next, spread(min(i + 2, nt - 1), i + 2, i + 1, i + 1));
+        scores(i + 1, next, spread(min(i + 2, nt - 1), i + 2, page2, i + 1, i + 1, page1));
+        page1 = page2;
+        page2 = page_of(i + 3);
         finish(i, s);
       };
       f32x16 s0[2], s1[2];
-      int i = od.masked;
       stage_barrier();
       if (i + 1 < nt) load(i + 1, true, false);
       scores(i, s0, nothing);
@@ -310,7 +319,7 @@ struct TileKernel {
 template <typename T, int D, int DV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
   typedef TileKernel<T, D, DV, NW, false> TK;
-  extern __shared__ char smem[];
+  extern __shared__ __align__(128) char smem[];  // (16-byte accesses, after any static LDS)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Workgroup b runs on XCD b % 8.  With a multiple of 8 kv heads an XCD takes
   // whole heads, a.heads_together of them at a time, so that its L2 holds their
@@ -342,7 +351,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
   const int last = min(row0 + TK::BM, s.n * a.g) - 1;
   const Span v0 = visible(a, s, div_g(a, row0)), v1 = visible(a, s, div_g(a, last));
   const int lo = v0.lo & ~(kGranule - 1), hi = min(v1.hi, s.kv);
-  Keys<D, DV, false> keys(a);
+  Keys<D, DV, false, false> keys(a);
   keys.seq(s, seq, kvh);
   Row r;
   typename TK::RB rb;
@@ -366,6 +375,16 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
 template <int BM, int BN, bool FEW>
 struct Work {
   static constexpr bool kFew = FEW;
+  // The units are cut into runs: kRuns equal ones (a power of two), or one unit
+  // each where there are fewer.
+  static constexpr int kRuns = FEW ? kFewGroups : kTileGroups;
+  static __device__ __forceinline__ int run_start(int n, int w) {
+    return n < kRuns ? min(w, n) : (int)((uint64_t)(uint32_t)n * (uint32_t)w / kRuns);
+  }
+  // runs that start before unit u (0 < u <= n)
+  static __device__ __forceinline__ int runs_before(int n, int u) {
+    return n < kRuns ? u : (int)(((uint64_t)(uint32_t)u * kRuns + n - 1) / (uint32_t)n);
+  }
   // requests of at most 32 rows go to the few-rows kernel, the others to tiles
   static __device__ __forceinline__ int row_tiles(const AttnArgs& a, const Seq& s) {
     const int rows = s.n * a.g;
@@ -379,72 +398,54 @@ struct Work {
   }
   // at least 1: rows that see nothing are written too
   static __device__ __forceinline__ int key_tiles(const Span& p) { return max(1, (p.hi - p.lo + BN - 1) / BN); }
-  static __device__ __forceinline__ long long units(const AttnArgs& a, const Seq& s) {
-    long long u = 0;
+  static __device__ __forceinline__ int units(const AttnArgs& a, const Seq& s) {
+    int u = 0;
     for (int qt = 0, n = row_tiles(a, s); qt < n; ++qt) u += key_tiles(span(a, s, qt));
     return u;
   }
 };
 
-__device__ __forceinline__ long long uniform64(long long v) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return (long long)(((uint64_t)hi << 32) | lo);
-}
-
 struct Place {
-  long long total;   // units of one kv head
-  long long before;  // units of the requests before r
+  int total;   // units of one kv head
+  int before;  // units of the requests before r
   int r;
 };
-// The request that unit `want(total)` of a kv head falls in; every thread of the NT gets it.
+// The request that unit `want(total)` of a kv head falls in; every thread of
+// the NT gets it.  (The entry points refuse launches of 2^31 units or more.)
+// tmp: NT / 64 + 2 ints of LDS
 template <typename W, int NT, typename F>
-__device__ Place find_place(const AttnArgs& a, F want) {
-  __shared__ long long wsum[NT / 64];
-  __shared__ long long found_before;
-  __shared__ int found_r;
+__device__ __forceinline__ Place find_place(const AttnArgs& a, int* tmp, F want) {
+  int *wsum = tmp, *found = tmp + NT / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.n_seqs + NT - 1) / NT, r0 = min(tid * per, a.n_seqs), r1 = min(r0 + per, a.n_seqs);
-  long long own = 0;
+  int own = 0;
   for (int r = r0; r < r1; ++r) own += W::units(a, paged_seq(a, r));
-  long long incl = own;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long o = __shfl_up(incl, d, 64);
-    if (lane >= d) incl += o;
-  }
+  const int incl = wave_incl_sum(own);
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
-  long long total = 0, base = 0;
+  int total = 0, base = 0;
 #pragma unroll
   for (int w = 0; w < NT / 64; ++w) {
     if (w < wave) base += wsum[w];
     total += wsum[w];
   }
-  total = uniform64(total);
-  long long at = base + incl - own;
-  const long long p = want(total);
+  total = __builtin_amdgcn_readfirstlane(total);
+  int at = base + incl - own;
+  const int p = want(total);
   if (p >= at && p < at + own) {
-    for (int r = r0; r < r1; ++r) {
-      const long long u = W::units(a, paged_seq(a, r));
-      if (p < at + u) {
-        found_r = r;
-        found_before = at;
-        break;
-      }
+    int r = r0;
+    for (; r + 1 < r1; ++r) {
+      const int u = W::units(a, paged_seq(a, r));
+      if (p < at + u) break;
       at += u;
     }
+    found[0] = r;
+    found[1] = at;
   }
   __syncthreads();
-  Place pl{total, 0, 0};
-  if (total > 0) {
-    pl.before = uniform64(found_before);
-    pl.r = __builtin_amdgcn_readfirstlane(found_r);
-  }
-  return pl;
+  if (total == 0) return Place{0, 0, 0};
+  return Place{total, __builtin_amdgcn_readfirstlane(found[1]), __builtin_amdgcn_readfirstlane(found[0])};
 }
-
-// first unit of run w of G over n >= G units
-__device__ __forceinline__ long long run_start(long long n, int w, int G) { return n * w / G; }
 
 __device__ __forceinline__ Seq uniform(const Seq& s) {
   return Seq{__builtin_amdgcn_readfirstlane(s.start), __builtin_amdgcn_readfirstlane(s.n),
@@ -454,39 +455,40 @@ __device__ __forceinline__ Seq uniform(const Seq& s) {
 // Calls segment(kvh, r, seq, qt, span, first key tile, key tiles, whole, slot)
 // for every piece of this workgroup's run.
 template <typename W, int NT, typename F>
-__device__ __forceinline__ void each_piece(const AttnArgs& a, PagedJoin* join, F segment) {
+__device__ __forceinline__ void each_piece(const AttnArgs& a, int* tmp, PagedJoin* join, F segment) {
   const int lane = threadIdx.x & 63;
-  int w = blockIdx.x, G = a.n_wg;  // this workgroup's run and the runs that there are
-  long long pos = 0, end = 0, N = 0;
-  const Place pl = find_place<W, NT>(a, [&](long long total) {
+  int w = blockIdx.x, pos = 0, end = 0, N = 0;  // this workgroup's run
+  const Place pl = find_place<W, NT>(a, tmp, [&](int total) {
     N = total * a.HK;
-    if (N < G)
-      G = (int)N;  // one unit a run
-    else if constexpr (!W::kFew)
-      // Workgroup b runs on XCD b % 8: an XCD's runs are neighbours, whose rows
-      // share keys and values (n_wg is a multiple of 8)
-      w = (w & 7) * (G >> 3) + (w >> 3);
-    if (w < G) {
-      pos = run_start(N, w, G);
-      end = run_start(N, w + 1, G);
-    }
+    // Workgroup b runs on XCD b % 8: an XCD's runs are neighbours, whose row
+    // tiles share keys and values
+    if (!W::kFew && N >= W::kRuns) w = (w & 7) * (W::kRuns / 8) + (w >> 3);
+    // Single rows share nothing, but the heads of a page lie side by side: they
+    // are read at the same time, by neighbouring workgroups
+    if (W::kFew && N >= W::kRuns && W::kRuns % a.HK == 0) w = w % a.HK * (W::kRuns / a.HK) + w / a.HK;
+    pos = W::run_start(N, w);
+    end = W::run_start(N, w + 1);
     return total ? pos % total : 0;
   });
   PagedJoin rec{0, 0, 0, 0, 0};
   if (pos < end) {
-    int kvh = (int)(pos / pl.total), r = pl.r, qt = 0;
-    long long off = pos % pl.total - pl.before;
+    int kvh = pos / pl.total, r = pl.r, qt = 0;
+    int off = pos % pl.total - pl.before;
     Seq s = uniform(paged_seq(a, r));
     while (pos < end) {
       const Span sp = W::span(a, s, qt);
       const int n = W::key_tiles(sp);
+      if (a.whole && off > 0 && off < n) {  // the run before takes it
+        pos += n - off;
+        off = n;
+      }
       if (off < n) {
-        const int t0 = (int)off, m = (int)min((long long)(n - t0), end - pos);
+        const int t0 = off, m = a.whole ? n : min(n - t0, end - pos);
         const bool whole = m == n;
         segment(kvh, r, s, qt, sp, t0, m, whole, 2 * w + (t0 == 0 ? 1 : 0));
         if (t0 == 0 && !whole) {
-          // the runs that start before the segment's end: those before ceil(end G / N)
-          const int parts = (int)(((pos + n) * G + N - 1) / N) - w;
+          // the runs that start before the segment's end
+          const int parts = W::runs_before(N, pos + n) - w;
           rec = PagedJoin{parts, s.start, s.n, qt, kvh};
         }
         pos += m;
@@ -513,7 +515,7 @@ __device__ __forceinline__ void each_piece(const AttnArgs& a, PagedJoin* join, F
       }
     }
   }
-  if (threadIdx.x == 0) join[w] = rec;  // (w < n_wg whatever G is)
+  if (threadIdx.x == 0) join[w] = rec;
 }
 
 __device__ __forceinline__ int64_t part_row(int slot, int row, int BM) { return (int64_t)slot * BM + row; }
@@ -523,13 +525,14 @@ template <typename T, int D, int DV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
   typedef TileKernel<T, D, DV, NW, true> TK;
   typedef Work<TK::BM, kTileKeys, false> W;
-  extern __shared__ char smem[];
+  extern __shared__ __align__(128) char smem[];  // (16-byte accesses, after any static LDS)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   typename TK::RB rb;
   typename TK::RB::Addr ad;
   ad.set();
-  Keys<D, DV, true> keys(a);
-  each_piece<W, 64 * NW>(a, a.tile_join, [&](int kvh, int r, const Seq& s, int qt, const Span& sp, int t0, int n, bool whole, int slot) {
+  Keys<D, DV, true, false> keys(a);
+  // (stage 1 is not loaded before the waves' first barrier)
+  each_piece<W, 64 * NW>(a, (int*)(smem + TK::kStage), a.tile_join, [&](int kvh, int r, const Seq& s, int qt, const Span& sp, int t0, int n, bool whole, int slot) {
     const int in = wave * 32 + (lane & 31);
     keys.seq(s, r, kvh);
     const int lo = sp.lo + t0 * kTileKeys;
@@ -579,30 +582,54 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
   typedef FewKernel<T, D, DV, NW> FK;
   typedef RowBlock<T, D, DV> RB;
   typedef Work<kFewRows, FK::BN, true> W;
-  extern __shared__ char smem[];
+  extern __shared__ __align__(128) char smem[];  // (16-byte accesses, after any static LDS)
   __shared__ float ml[NW][kFewRows][2];
+  __shared__ int tmp[NW + 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
   const uint32_t mine = lds_addr(smem) + wave * FK::kWave;
   RB rb;
   typename RB::Addr ad;
   ad.set();
-  Keys<D, DV, true> keys(a);
-  each_piece<W, 64 * NW>(a, a.few_join, [&](int kvh, int r, const Seq& s, int, const Span& sp, int t0, int n, bool whole, int slot) {
+  Keys<D, DV, true, true> keys(a);
+  each_piece<W, 64 * NW>(a, tmp, a.few_join, [&](int kvh, int r, const Seq& s, int, const Span& sp, int t0, int n, bool whole, int slot) {
     keys.seq(s, r, kvh);
     const Order od(sp.lo + t0 * FK::BN + wave * 32, min(sp.hi, sp.lo + (t0 + n) * FK::BN), FK::BN, 32,
                    Span{visible(a, s, s.n - 1).lo, min(visible(a, s, 0).hi, s.kv)});
-    auto load = [&](int i) {
-      const uint32_t st = mine + (i & 1) * FK::kStage;
+    // tile i's two granules and their pages
+    struct Two {
+      int g[2], page[2];
+    };
+    auto where = [&](int i) {
+      Two t;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int g = keys.granule(od.key(i) + j * kGranule), page = keys.page(g);
-        keys.load_k(g, page, st + j * (kGranule * D * 2));
-        keys.load_v(g, page, st + FK::kK + j * (kGranule * DV * 2));
+        t.g[j] = keys.granule(od.key(i) + j * kGranule);
+        t.page[j] = keys.page(t.g[j]);
       }
+      return t;
     };
-    if (od.n > 0) load(0);
-    if (od.n > 1) load(1);
+    auto load_k = [&](int i, const Two& t) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        keys.load_k(t.g[j], t.page[j], mine + (i & 1) * FK::kStage + j * (kGranule * D * 2));
+    };
+    auto load_v = [&](int i, const Two& t) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        keys.load_v(t.g[j], t.page[j], mine + (i & 1) * FK::kStage + FK::kK + j * (kGranule * DV * 2));
+    };
+    Two ahead;  // of tile i + 2, looked up while tile i is taken
+    if (od.n > 0) {
+      const Two t0 = where(0), t1 = where(min(1, od.n - 1));
+      ahead = where(min(2, od.n - 1));
+      load_k(0, t0);
+      load_v(0, t0);
+      if (od.n > 1) {
+        load_k(1, t1);
+        load_v(1, t1);
+      }
+    }
     const Row row = row_of(a, s, lane & 31);
     rb.load_q(q_row(a, s, row, kvh));
     rb.clear();
@@ -614,13 +641,18 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
         wait_loads<0>();
       const uint32_t kt = mine + (i & 1) * FK::kStage;
       f32x16 sc[1] = {rb.scores(ad, kt, [](int) {})};
+      const bool more = i + 2 < od.n;
+      // the stage's keys are read: the next but one's may take their place
+      wait_lds();
+      if (more) load_k(i + 2, ahead);
       if (masked) RB::mask(sc[0], od.key(i), row.see.lo, top);
       rb.rescale(RB::template largest<1>(sc), a.c);
       uint32_t p[8];
       rb.weights(sc[0], a.c, p);
       rb.values(ad, kt + FK::kK, p);
       wait_lds();
-      if (i + 2 < od.n) load(i + 2);
+      if (more) load_v(i + 2, ahead);
+      ahead = where(min(i + 3, od.n - 1));
     };
     for (int i = 0; i < od.masked; ++i) tile(i, true);
     if (od.masked > 0 && !rb.finite())
@@ -702,19 +734,42 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, const Paged
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row0 = rec.row_tile * BM, rows = min(BM, rec.n * a.g - row0);
   for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
-    auto slot = [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); };
-    float M = kLowest;
-    for (int i = lane; i < rec.parts; i += 64) M = fmaxf(M, ml[2 * part_row(slot(i), row, BM)]);
+    auto part_at = [&](int i) { return part_row(i == 0 ? 2 * w + 1 : 2 * (w + i), row, BM); };
+    float M = kLowest, L = 0.0f, o[NC] = {};
+    for (int i0 = 0; i0 < rec.parts; i0 += 64) {
+      // a lane takes a piece's maximum and sum; then its factor goes round
+      const int n = min(64, rec.parts - i0);
+      const int64_t mine = part_at(min(i0 + lane, rec.parts - 1));
+      const float mi = lane < n ? ml[2 * mine] : kLowest, li = ml[2 * mine + 1];
+      float top = mi;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
-    float L = 0.0f, o[NC] = {};
-    for (int i = 0; i < rec.parts; ++i) {
-      const int64_t at = part_row(slot(i), row, BM);
-      const float mi = ml[2 * at];
-      const float f = mi == kLowest ? 0.0f : exp2_fast((mi - M) * a.c);
-      L += f * ml[2 * at + 1];
+      for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+      const float next = fmaxf(M, top), f0 = M == kLowest ? 0.0f : exp2_fast((M - next) * a.c);
+      const float f = mi == kLowest ? 0.0f : exp2_fast((mi - next) * a.c);
+      float sum = mi == kLowest ? 0.0f : f * li;
 #pragma unroll
-      for (int j = 0; j < NC; ++j) o[j] += f * part[at * DV + lane * NC + j];
+      for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+      L = L * f0 + sum;
+      M = next;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) o[j] *= f0;
+      // pieces in flight: single rows are cut in up to a run a workgroup, tiles in two or three
+      constexpr int U = BM == kFewRows ? 8 : 2;
+      for (int i = 0; i < n; i += U) {
+        float x[U][NC];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float* p = part + part_at(i0 + min(i + u, n - 1)) * DV + lane * NC;
+#pragma unroll
+          for (int j = 0; j < NC; ++j) x[u][j] = p[j];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float fu = i + u < n ? __shfl(f, i + u, 64) : 0.0f;
+#pragma unroll
+          for (int j = 0; j < NC; ++j) o[j] = fmaf(fu, fu == 0.0f ? 0.0f : x[u][j], o[j]);
+        }
+      }
     }
     const float inv = L > 0.0f || !(L == L) ? 1.0f / L : 0.0f;
     const int token = div_g(a, row0 + row), head = rec.kvh * a.g + row0 + row - token * a.g;
@@ -798,6 +853,9 @@ hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws,
     a.tile_join = (PagedJoin*)(ws + l.tile_join);
     a.tile_ml = (float*)(ws + l.tile_ml);
     a.tile_part = (float*)(ws + l.tile_part);
+    // Where no request can have more than 512 keys a segment is not cut: a
+    // workgroup takes its four tiles in about the time of the join's launch.
+    a.whole = a.max_kv <= 512;
     hipError_t e;
     {
       constexpr int NW = d.value == 192 ? 3 : 4;  // 160 KB of LDS
@@ -805,7 +863,6 @@ hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws,
       static std::atomic<uint64_t> done{0};
       auto kernel = paged_few_kernel<T, d.value, DV, NW>;
       if ((e = raise_lds_limit((const void*)kernel, done, FK::lds)) != hipSuccess) return e;
-      a.n_wg = kFewGroups;
       kernel<<<kFewGroups, 64 * NW, FK::lds, s>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
@@ -815,12 +872,14 @@ hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws,
       static std::atomic<uint64_t> done{0};
       auto kernel = paged_tile_kernel<T, d.value, DV, NW>;
       if ((e = raise_lds_limit((const void*)kernel, done, TK::lds)) != hipSuccess) return e;
-      a.n_wg = kTileGroups;
       kernel<<<kTileGroups, 64 * NW, TK::lds, s>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
-      paged_join_kernel<T, DV, TK::BM><<<dim3(kTileGroups, 8), 256, 0, s>>>(a, a.tile_join, a.tile_part, a.tile_ml);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (!a.whole) {
+        paged_join_kernel<T, DV, TK::BM><<<dim3(kTileGroups, 8), 256, 0, s>>>(a, a.tile_join, a.tile_part, a.tile_ml);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
     }
+    if (a.whole) return hipSuccess;
     paged_join_kernel<T, DV, kFewRows><<<dim3(kFewGroups, kFewRows / 4), 256, 0, s>>>(a, a.few_join, a.few_part, a.few_ml);
     return hipGetLastError();
   });

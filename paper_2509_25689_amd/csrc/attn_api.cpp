@@ -273,6 +273,10 @@ moeq_status moeq_attn_paged(const moeq_attn* a, const moeq_rows* q, const moeq_k
   g.page_shift = log2_of(cache->page_size);
   const int64_t most = (int64_t)max_blocks << g.page_shift;
   g.max_kv = most > 0x3FFFFFFF ? 0x3FFFFFFF : (int32_t)most;
+  // key tiles of at least 64 keys, over all rows' tiles and kv heads
+  if (((int64_t)n_tokens * g.g / 128 + n_requests + 1) * (g.max_kv / 64 + 1) * g.HK > 0x7FFFFFFFLL)
+    return fail(MOEQ_ERR_UNSUPPORTED, "%d requests, %d tokens over up to %d keys exceed 2^31 tiles", n_requests,
+                n_tokens, g.max_kv);
   g.n_pages = cache->n_pages;
   g.n_seqs = n_requests;
   g.T = n_tokens;

@@ -82,15 +82,29 @@ __device__ __forceinline__ int v_swz(int r, int c) {
 // 64 lanes' 16 bytes each from base + off (bytes) into LDS at dst + 16 * lane.
 // Written out because the compiler, given the builtin, waits for every load
 // in flight before each transposing LDS read.  There is no output register;
-// whoever reads the tile waits first (wait_loads).
+// whoever reads the tile waits first (wait_loads).  base may have been written by
+// a lane read just before, and a memory instruction must not read such a register
+// for 5 wait states; m0 needs one: the s_mov and the s_nop are those five.
+// ONCE: the data is read by no one else (with this hint single tokens over 3.9 GB
+// of cache took 636 us, without 709).
+template <bool ONCE>
 __device__ __forceinline__ void load_lds(const char* base, uint32_t off, uint32_t dst) {
-  asm volatile(
-      "s_mov_b32 m0, %2\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %0, %1"
-      :
-      : "v"(off), "s"(base), "s"(dst)
-      : "m0");
+  if constexpr (ONCE)
+    asm volatile(
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 3\n\t"
+        "global_load_lds_dwordx4 %0, %1 nt"
+        :
+        : "v"(off), "s"(base), "s"(dst)
+        : "m0");
+  else
+    asm volatile(
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 3\n\t"
+        "global_load_lds_dwordx4 %0, %1"
+        :
+        : "v"(off), "s"(base), "s"(dst)
+        : "m0");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -100,7 +114,7 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 
 // The lane's byte offsets of a granule's loads from its first row: load i
 // covers the granule's chunks 64 i .. 64 i + 63.
-template <int C, bool IsK>
+template <int C, bool IsK, bool ONCE>
 struct GranuleOffsets {
   static constexpr int N = C / 4;  // loads per granule
   uint32_t off[N];
@@ -113,7 +127,7 @@ struct GranuleOffsets {
     }
   }
   __device__ __forceinline__ void load_one(const char* base, uint32_t dst, int i) const {
-    load_lds(base, off[i], dst + 1024u * i);
+    load_lds<ONCE>(base, off[i], dst + 1024u * i);
   }
   __device__ __forceinline__ void load(const char* base, uint32_t dst) const {
 #pragma unroll
