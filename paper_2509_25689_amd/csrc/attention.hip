@@ -268,8 +268,9 @@ struct TileKernel {
     if (od.masked > 0 && !rb.finite())
       rb.redo(a.c, r.see.lo, min(r.see.hi, keys.kv), od.masked, kTileKeys, hi, [&](int i) { return od.key(i); },
               [&](int key) { return keys.key_row(key); }, [&](int key) { return keys.value_row(key); });
-    if constexpr (D > 128) {
-      // (the scores of two tiles do not fit the registers beside 192-wide queries)
+    if constexpr (PAGED && D > 128) {
+      // (the scores of two tiles do not fit the registers beside 192-wide queries
+      // and the pages' state)
       int page1 = od.masked < nt ? page_of(od.masked + 1) : 0;
       for (int i = od.masked; i < nt; ++i) {
         stage_barrier();
@@ -405,21 +406,29 @@ struct Work {
   }
 };
 
+__device__ __forceinline__ Seq uniform(const Seq& s) {
+  return Seq{__builtin_amdgcn_readfirstlane(s.start), __builtin_amdgcn_readfirstlane(s.n),
+             __builtin_amdgcn_readfirstlane(s.kv)};
+}
+
 struct Place {
-  int total;   // units of one kv head
-  int before;  // units of the requests before r
-  int r;
+  int total;  // units of one kv head
+  int kvh, r, off;  // kv head and request that the unit falls in, and its number among the request's
+  Seq seq;
 };
-// The request that unit `want(total)` of a kv head falls in; every thread of
-// the NT gets it.  (The entry points refuse launches of 2^31 units or more.)
-// tmp: NT / 64 + 2 ints of LDS
+// Where unit `want(total)` falls; every thread of the NT gets it.  (The entry
+// points refuse launches of 2^31 units or more.)  tmp: NT / 64 + 5 ints of LDS
 template <typename W, int NT, typename F>
 __device__ __forceinline__ Place find_place(const AttnArgs& a, int* tmp, F want) {
   int *wsum = tmp, *found = tmp + NT / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.n_seqs + NT - 1) / NT, r0 = min(tid * per, a.n_seqs), r1 = min(r0 + per, a.n_seqs);
   int own = 0;
-  for (int r = r0; r < r1; ++r) own += W::units(a, paged_seq(a, r));
+  Seq mine{0, 0, 0};  // the last of this thread's requests: the only one of up to NT
+  for (int r = r0; r < r1; ++r) {
+    mine = paged_seq(a, r);
+    own += W::units(a, mine);
+  }
   const int incl = wave_incl_sum(own);
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
@@ -431,25 +440,26 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, int* tmp, F want)
   }
   total = __builtin_amdgcn_readfirstlane(total);
   int at = base + incl - own;
-  const int p = want(total);
+  const int u = want(total), kvh = total ? u / total : 0, p = u - kvh * total;
   if (p >= at && p < at + own) {
     int r = r0;
-    for (; r + 1 < r1; ++r) {
-      const int u = W::units(a, paged_seq(a, r));
-      if (p < at + u) break;
-      at += u;
-    }
+    if (per > 1)
+      for (;; ++r) {
+        mine = paged_seq(a, r);
+        const int n = W::units(a, mine);
+        if (p < at + n) break;
+        at += n;
+      }
     found[0] = r;
-    found[1] = at;
+    found[1] = p - at;
+    found[2] = mine.start;
+    found[3] = mine.n;
+    found[4] = mine.kv;
   }
   __syncthreads();
-  if (total == 0) return Place{0, 0, 0};
-  return Place{total, __builtin_amdgcn_readfirstlane(found[1]), __builtin_amdgcn_readfirstlane(found[0])};
-}
-
-__device__ __forceinline__ Seq uniform(const Seq& s) {
-  return Seq{__builtin_amdgcn_readfirstlane(s.start), __builtin_amdgcn_readfirstlane(s.n),
-             __builtin_amdgcn_readfirstlane(s.kv)};
+  if (total == 0) return Place{0, 0, 0, 0, Seq{0, 0, 0}};
+  return Place{total, kvh, __builtin_amdgcn_readfirstlane(found[0]), __builtin_amdgcn_readfirstlane(found[1]),
+               uniform(Seq{found[2], found[3], found[4]})};
 }
 
 // Calls segment(kvh, r, seq, qt, span, first key tile, key tiles, whole, slot)
@@ -468,13 +478,12 @@ __device__ __forceinline__ void each_piece(const AttnArgs& a, int* tmp, PagedJoi
     if (W::kFew && N >= W::kRuns && W::kRuns % a.HK == 0) w = w % a.HK * (W::kRuns / a.HK) + w / a.HK;
     pos = W::run_start(N, w);
     end = W::run_start(N, w + 1);
-    return total ? pos % total : 0;
+    return pos;
   });
   PagedJoin rec{0, 0, 0, 0, 0};
   if (pos < end) {
-    int kvh = pos / pl.total, r = pl.r, qt = 0;
-    int off = pos % pl.total - pl.before;
-    Seq s = uniform(paged_seq(a, r));
+    int kvh = pl.kvh, r = pl.r, qt = 0, off = pl.off;
+    Seq s = pl.seq;
     while (pos < end) {
       const Span sp = W::span(a, s, qt);
       const int n = W::key_tiles(sp);
@@ -584,7 +593,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
   typedef Work<kFewRows, FK::BN, true> W;
   extern __shared__ __align__(128) char smem[];  // (16-byte accesses, after any static LDS)
   __shared__ float ml[NW][kFewRows][2];
-  __shared__ int tmp[NW + 2];
+  __shared__ int tmp[NW + 5];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5;
   const uint32_t mine = lds_addr(smem) + wave * FK::kWave;
