@@ -347,7 +347,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
   }
   seq = __builtin_amdgcn_readfirstlane(seq);
   const Seq s = prompt_seq(a, seq);
-  const int row0 = (slot - __builtin_amdgcn_readfirstlane(first_slot(seq))) * TK::BM;
+  const int row0 = (slot - ((int)((int64_t)s.start * a.g / TK::BM) + seq)) * TK::BM;
   if (row0 < 0 || row0 >= s.n * a.g) return;
   const int last = min(row0 + TK::BM, s.n * a.g) - 1;
   const Span v0 = visible(a, s, div_g(a, row0)), v1 = visible(a, s, div_g(a, last));
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
 // The work of a launch is the key tiles of all (kv head, request, row tile)
 // segments one after another, cut into equal runs for the workgroups whatever
 // the lengths: a segment that one workgroup holds whole is written directly,
-// pieces of one leave partial sums that paged_join_kernel adds up.  A workgroup
+// pieces of one leave partial sums that a join kernel adds up.  A workgroup
 // leaves at most two: the piece it starts with (slot 2 w) and the one it ends
 // with (slot 2 w + 1).
 template <int BM, int BN, bool FEW>
@@ -527,7 +527,15 @@ __device__ __forceinline__ void each_piece(const AttnArgs& a, int* tmp, PagedJoi
   if (threadIdx.x == 0) join[w] = rec;
 }
 
-__device__ __forceinline__ int64_t part_row(int slot, int row, int BM) { return (int64_t)slot * BM + row; }
+// A piece's sums of tiled rows lie as a wave's registers do: a wave's `at` (slot
+// times waves, plus its own number), 16 bytes a lane a store; maxima and sums by row.
+template <int DV>
+__device__ __forceinline__ f32x4* tile_part(const AttnArgs& a, int at) {
+  return (f32x4*)a.tile_part + (int64_t)at * (DV / 8) * 64 + (threadIdx.x & 63);
+}
+__device__ __forceinline__ f32x2v* tile_ml(const AttnArgs& a, int at) {
+  return (f32x2v*)a.tile_ml + (int64_t)at * 32 + (threadIdx.x & 31);
+}
 
 // requests of more than 32 rows
 template <typename T, int D, int DV, int NW>
@@ -556,19 +564,13 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
     const float l = sum_halves(rb.l);
     if (whole) {
       store_out<T, DV>(a, rb.o, rb.m, l, s, row, kvh);
-    } else if (row.valid) {
-      const int64_t at = part_row(slot, in, TK::BM);
-      const int h = lane >> 5;
+    } else {
+      f32x4* part = tile_part<DV>(a, slot * NW + wave);
 #pragma unroll
-      for (int b = 0; b < TK::RB::DB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *(f32x4*)(a.tile_part + at * DV + 32 * b + 2 * i + 4 * h) =
-              f32x4{rb.o[b][i], rb.o[b][i + 1], rb.o[b][i + 2], rb.o[b][i + 3]};
-      if (h == 0) {
-        a.tile_ml[2 * at] = rb.m;
-        a.tile_ml[2 * at + 1] = l;
-      }
+      for (int i = 0; i < DV / 8; ++i)
+        part[i * 64] = f32x4{rb.o[i / 4][4 * (i % 4)], rb.o[i / 4][4 * (i % 4) + 1], rb.o[i / 4][4 * (i % 4) + 2],
+                             rb.o[i / 4][4 * (i % 4) + 3]};
+      if (lane < 32) *tile_ml(a, slot * NW + wave) = f32x2v{rb.m, l};
     }
   });
 }
@@ -718,7 +720,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
         if (a.lse && col == 0)
           a.lse[(int64_t)(s.start + token) * a.HQ + head] = m == kLowest ? -INFINITY : m * a.scale + __logf(lr);
       } else {
-        const int64_t at = part_row(slot, rr, kFewRows);
+        const int64_t at = (int64_t)slot * kFewRows + rr;
         *(f32x4*)(a.few_part + at * DV + col) = x;
         *(f32x4*)(a.few_part + at * DV + col + 4) = y;
         if (col == 0) {
@@ -731,19 +733,63 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
   });
 }
 
-// Adds up the pieces of the segments that were cut: workgroup (w, y), wave by
-// row; one wave a row, DV / 64 columns a lane.
-template <typename T, int DV, int BM>
-__global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, const PagedJoin* join, const float* part,
-                                                        const float* ml) {
+// The pieces of the segment that run w begins: its own, the next runs' first ones.
+__device__ __forceinline__ int piece_slot(int w, int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); }
+
+// Adds up the pieces of cut segments: of tiled rows, one workgroup a segment,
+// each wave its 32 rows, in the registers' order.
+template <typename T, int DV, int NW>
+__global__ __launch_bounds__(64 * NW) void tile_join_kernel(AttnArgs a) {
+  const int w = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const PagedJoin rec = a.tile_join[w];
+  if (rec.parts == 0) return;
+  const Seq s{rec.start, rec.n, 0};
+  Row r;
+  const int row = (rec.row_tile * NW + wave) * 32 + (lane & 31);
+  r.valid = row < rec.n * a.g;
+  r.token = div_g(a, row);
+  r.head = row - r.token * a.g;
+  f32x16 o[DV / 32];
+#pragma unroll
+  for (int b = 0; b < DV / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
+  float M = kLowest, L = 0.0f;
+  for (int i = 0; i < rec.parts; ++i) {
+    const int at = piece_slot(w, i) * NW + wave;
+    const f32x4* part = tile_part<DV>(a, at);
+    const f32x2v ml = *tile_ml(a, at);
+    f32x4 x[DV / 8];
+#pragma unroll
+    for (int j = 0; j < DV / 8; ++j) x[j] = part[j * 64];
+    const float next = fmaxf(M, ml[0]);
+    const float f0 = M == kLowest ? 0.0f : exp2_fast((M - next) * a.c);
+    const float f = ml[0] == kLowest ? 0.0f : exp2_fast((ml[0] - next) * a.c);
+#pragma unroll
+    for (int j = 0; j < DV / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float& v = ((float*)&o[j / 4])[4 * (j % 4) + e];
+        v = fmaf(f, x[j][e], f0 * v);
+      }
+    L = fmaf(f, ml[1], f0 * L);
+    M = next;
+  }
+  store_out<T, DV>(a, o, M, L, s, r, rec.kvh);
+}
+
+// Of single rows: workgroup (w, y), one wave a row, DV / 64 columns a lane.
+template <typename T, int DV>
+__global__ __launch_bounds__(256) void few_join_kernel(AttnArgs a) {
   constexpr int NC = DV / 64;
   const int w = blockIdx.x;
-  const PagedJoin rec = join[w];
+  const PagedJoin rec = a.few_join[w];
   if (rec.parts == 0) return;
+  const float *part = a.few_part, *ml = a.few_ml;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = rec.row_tile * BM, rows = min(BM, rec.n * a.g - row0);
+  const int rows = rec.n * a.g;
   for (int row = blockIdx.y * 4 + wave; row < rows; row += 4 * gridDim.y) {
-    auto part_at = [&](int i) { return part_row(i == 0 ? 2 * w + 1 : 2 * (w + i), row, BM); };
+    auto part_at = [&](int i) { return (int64_t)piece_slot(w, i) * kFewRows + row; };
     float M = kLowest, L = 0.0f, o[NC] = {};
     for (int i0 = 0; i0 < rec.parts; i0 += 64) {
       // a lane takes a piece's maximum and sum; then its factor goes round
@@ -762,8 +808,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, const Paged
       M = next;
 #pragma unroll
       for (int j = 0; j < NC; ++j) o[j] *= f0;
-      // pieces in flight: single rows are cut in up to a run a workgroup, tiles in two or three
-      constexpr int U = BM == kFewRows ? 8 : 2;
+      constexpr int U = 8;  // pieces in flight (up to a run of every workgroup)
       for (int i = 0; i < n; i += U) {
         float x[U][NC];
 #pragma unroll
@@ -781,7 +826,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttnArgs a, const Paged
       }
     }
     const float inv = L > 0.0f || !(L == L) ? 1.0f / L : 0.0f;
-    const int token = div_g(a, row0 + row), head = rec.kvh * a.g + row0 + row - token * a.g;
+    const int token = div_g(a, row), head = rec.kvh * a.g + row - token * a.g;
     char* out = a.out + (int64_t)(rec.start + token) * a.o_row + (int64_t)head * a.o_head;
     const uint32_t u = T::pack(o[0] * inv, o[NC - 1] * inv);
     if constexpr (NC == 2)
@@ -884,12 +929,12 @@ hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws,
       kernel<<<kTileGroups, 64 * NW, TK::lds, s>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       if (!a.whole) {
-        paged_join_kernel<T, DV, TK::BM><<<dim3(kTileGroups, 8), 256, 0, s>>>(a, a.tile_join, a.tile_part, a.tile_ml);
+        tile_join_kernel<T, DV, NW><<<kTileGroups, 64 * NW, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
       }
     }
     if (a.whole) return hipSuccess;
-    paged_join_kernel<T, DV, kFewRows><<<dim3(kFewGroups, kFewRows / 4), 256, 0, s>>>(a, a.few_join, a.few_part, a.few_ml);
+    few_join_kernel<T, DV><<<dim3(kFewGroups, kFewRows / 4), 256, 0, s>>>(a);
     return hipGetLastError();
   });
 }
