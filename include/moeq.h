@@ -534,7 +534,8 @@ moeq_status moeq_kv_append(const moeq_attn* a, const moeq_kv_cache* cache, const
  * cu[s + 1] - 1 are sequence s and see each other only.
  *   q, k, v   DEVICE rows [n_tokens x heads x dims]
  *   cu        DEVICE int32 [n_seqs + 1], ascending, within 0 .. n_tokens
- *   out       DEVICE rows [n_tokens x n_heads x value_dim] (written)
+ *   out       DEVICE rows [n_tokens x n_heads x value_dim] (written), apart from
+ *             each other and from q, k and v
  *   lse       DEVICE float [n_tokens x n_heads] (written): natural logarithm of
  *             each row's sum of exponentials; or NULL
  * Tokens of no sequence are not written.

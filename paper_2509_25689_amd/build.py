@@ -2,8 +2,9 @@
 
 Every source under ``csrc/`` is compiled with hipcc (one process per file, in
 parallel) and linked into ``paper_2509_25689_amd/libmoeq.so``; ``peaks/`` (the
-benchmark's measured roofline denominators) into ``libmoeq_peaks.so``.  Always
-recompiles: this is the "does it build" step."""
+benchmark's measured roofline denominators) into ``libmoeq_peaks.so``; the
+attention operators' binding to torch (host code, g++) into ``_attention.so``
+beside them.  Always recompiles: this is the "does it build" step."""
 import concurrent.futures
 import os
 import shutil
@@ -15,6 +16,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmoeq.so")
+BINDING = os.path.join(PKG, "binding", "attention.cpp")
+BINDING_LIB = os.path.join(PKG, "_attention.so")
 PEAKS = os.path.join(PKG, "peaks")
 PEAKS_LIB = os.path.join(PKG, "libmoeq_peaks.so")
 ARCH = "gfx950"
@@ -53,6 +56,35 @@ def _link(objs, lib):
     os.replace(tmp, lib)
 
 
+def _compile_binding():
+    """The attention operators' binding to torch: host code only, so that a call
+    costs the interpreter one step."""
+    import sysconfig
+    import torch
+    tdir = os.path.join(os.path.dirname(torch.__file__), "include")
+    obj = os.path.join(BUILD, "binding_attention.o")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-c", BINDING, "-o", obj,
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-isystem", tdir, "-isystem", os.path.join(tdir, "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"]]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    return obj
+
+
+def _link_binding(obj):
+    import torch
+    tlib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = BINDING_LIB + ".tmp"
+    cmd = [shutil.which("g++") or "g++", "-shared", obj, "-o", tmp, "-L", tlib, "-ltorch_python", "-ltorch", "-ltorch_cpu",
+           "-lc10", "-L", PKG, "-l:libmoeq.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, BINDING_LIB)
+
+
 def _sources(d):
     return sorted(os.path.join(d, f) for f in os.listdir(d) if f.endswith((".hip", ".cpp")))
 
@@ -61,12 +93,14 @@ def build(verbose=False):
     os.makedirs(BUILD, exist_ok=True)
     srcs = _sources(CSRC)
     psrcs = _sources(PEAKS)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + len(psrcs))) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + len(psrcs) + 1)) as ex:
+        binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, srcs + psrcs))
     _link(objs[:len(srcs)], LIB)
     _link(objs[len(srcs):], PEAKS_LIB)
+    _link_binding(binding.result())
     if verbose:
-        print(f"built {LIB} and {PEAKS_LIB}")
+        print(f"built {LIB}, {PEAKS_LIB} and {BINDING_LIB}")
     return LIB
 
 

@@ -76,6 +76,16 @@ moeq_status check_rows(const moeq_rows* r, const char* name, bool neighbours) {
   return MOEQ_OK;
 }
 
+// rows that are written: no two at the same place
+moeq_status check_out(const moeq_rows* r, int64_t tokens, const moeq_attn* a) {
+  const moeq_status st = check_rows(r, "out", false);
+  if (st != MOEQ_OK) return st;
+  if ((tokens > 1 && r->token_stride < a->value_dim) || (a->n_heads > 1 && r->head_stride < a->value_dim))
+    return fail(MOEQ_ERR_INVALID_ARG, "out: rows %lld and %lld elements apart overlap", (long long)r->token_stride,
+                (long long)r->head_stride);
+  return MOEQ_OK;
+}
+
 moeq_status check_pages(int32_t page_size, int32_t n_pages) {
   if (page_size < 16 || page_size > 4096 || (page_size & (page_size - 1)))
     return fail(MOEQ_ERR_INVALID_ARG, "page_size %d must be a power of two, 16 .. 4096", page_size);
@@ -194,7 +204,7 @@ moeq_status moeq_attn_prompt(const moeq_attn* a, const moeq_rows* q, const moeq_
   if ((st = check_counts(a, n_seqs, n_tokens, "n_seqs")) != MOEQ_OK) return st;
   if (n_seqs == 0 || n_tokens == 0) return MOEQ_OK;
   if ((st = check_rows(q, "q", false)) != MOEQ_OK || (st = check_rows(k, "k", true)) != MOEQ_OK ||
-      (st = check_rows(v, "v", true)) != MOEQ_OK || (st = check_rows(out, "out", false)) != MOEQ_OK)
+      (st = check_rows(v, "v", true)) != MOEQ_OK || (st = check_out(out, n_tokens, a)) != MOEQ_OK)
     return st;
   if (!cu || !aligned4(cu) || !aligned4(lse))
     return fail(MOEQ_ERR_INVALID_ARG, "cu must not be NULL; cu and lse must be 4-byte aligned");
@@ -240,7 +250,7 @@ moeq_status moeq_attn_paged(const moeq_attn* a, const moeq_rows* q, const moeq_k
   if (max_blocks < 1 || table_stride < max_blocks)
     return fail(MOEQ_ERR_INVALID_ARG, "max_blocks %d must be positive and at most table_stride", max_blocks);
   if (n_requests == 0 || n_tokens == 0 || max_new == 0) return MOEQ_OK;
-  if ((st = check_rows(q, "q", false)) != MOEQ_OK || (st = check_rows(out, "out", false)) != MOEQ_OK) return st;
+  if ((st = check_rows(q, "q", false)) != MOEQ_OK || (st = check_out(out, n_tokens, a)) != MOEQ_OK) return st;
   if (!cu_q || !kv_lens || !block_table || !aligned4(cu_q) || !aligned4(kv_lens) || !aligned4(block_table) ||
       !aligned4(lse))
     return fail(MOEQ_ERR_INVALID_ARG, "cu_q, kv_lens and block_table must not be NULL; these and lse 4-byte aligned");

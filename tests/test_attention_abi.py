@@ -58,6 +58,7 @@ def test_prompt_arguments():
             assert _prompt(**{name: r}) == BAD, name
             assert name in moeq.moeq_last_error()
     assert _prompt(k=_rows(t=1 << 26)) == BAD
+    assert _prompt(out=_rows(t=0)) == BAD and _prompt(out=_rows(h=64)) == BAD   # rows that overlap
     assert _prompt(cu=None) == BAD and _prompt(cu=FAKE + 2) == BAD and _prompt(lse=FAKE + 1) == BAD
     assert _prompt(seqs=-1) == BAD and _prompt(tokens=-1) == BAD and _prompt(tokens=(1 << 24) + 1) == BAD
     assert _prompt(_attn(n_heads=256, n_kv_heads=256), tokens=1 << 24) == UNSUP
