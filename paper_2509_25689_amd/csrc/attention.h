@@ -6,6 +6,25 @@
 
 namespace moeq {
 
+namespace {
+
+// Sums of non-negative numbers that stop at 2^31 - 1 (and so stay monotone)
+__device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int add_dpp(int v) {
+  return add_sat(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, false));
+}
+__device__ __forceinline__ int wave_incl_sat(int v) {
+  v = add_dpp<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v = add_dpp<0x112, 0xF>(v);
+  v = add_dpp<0x114, 0xF>(v);
+  v = add_dpp<0x118, 0xF>(v);
+  v = add_dpp<0x142, 0xA>(v);  // row_bcast 15, 31
+  return add_dpp<0x143, 0xC>(v);
+}
+
+}  // namespace
+
 constexpr int kFewRows = 32;      // rows of a request that the few-rows kernel takes
 constexpr int kFewGroups = 256;   // its workgroups: one per compute unit
 constexpr int kTileGroups = 512;  // workgroups of the tile kernel over the cache: two per compute unit

@@ -6,7 +6,6 @@
 
 #include "attention.h"
 #include "attn_core.h"
-#include "route_wave.h"
 
 namespace moeq {
 
@@ -140,6 +139,12 @@ __device__ __forceinline__ const char* q_row(const AttnArgs& a, const Seq& s, co
   return r.valid ? a.q + (int64_t)(s.start + r.token) * a.q_row + (int64_t)(kvh * a.g + r.head) * a.q_head : nullptr;
 }
 
+// A row without keys has m = kLowest and l = 0.  (Scores that are all NaN leave m
+// there too, but l is NaN: where rows' parts are joined, l says whether there is one.)
+__device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
+  return l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
+}
+
 template <typename T, int DV, int DB>
 __device__ __forceinline__ void store_out(const AttnArgs& a, const f32x16 (&o)[DB], float m, float l, const Seq& s,
                                           const Row& r, int kvh) {
@@ -164,7 +169,7 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const f32x16 (&o)[D
       if (r.valid) *(u32x4*)(row + (32 * b + 16 * t + 8 * h) * 2) = u32x4{u[0], w[0], u[1], w[1]};
     }
   if (a.lse && r.valid && h == 0)
-    a.lse[(int64_t)(s.start + r.token) * a.HQ + head] = m == kLowest ? -INFINITY : m * a.scale + __logf(l);
+    a.lse[(int64_t)(s.start + r.token) * a.HQ + head] = log_sum(a, m, l);
 }
 
 // The order in which the key tiles of [lo, hi) are taken, `width` keys each, the
@@ -427,19 +432,21 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, int* tmp, F want)
   Seq mine{0, 0, 0};  // the last of this thread's requests: the only one of up to NT
   for (int r = r0; r < r1; ++r) {
     mine = paged_seq(a, r);
-    own += W::units(a, mine);
+    own = add_sat(own, W::units(a, mine));
   }
-  const int incl = wave_incl_sum(own);
+  const int incl = wave_incl_sat(own);
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
   int total = 0, base = 0;
 #pragma unroll
   for (int w = 0; w < NT / 64; ++w) {
-    if (w < wave) base += wsum[w];
-    total += wsum[w];
+    if (w < wave) base = add_sat(base, wsum[w]);
+    total = add_sat(total, wsum[w]);
   }
   total = __builtin_amdgcn_readfirstlane(total);
-  int at = base + incl - own;
+  // (lengths that ascend stay below; with others nothing is done)
+  if ((uint64_t)(uint32_t)total * (uint32_t)a.HK >= 0x7FFFFFFFu) total = 0;
+  int at = add_sat(base, incl) - own;
   const int u = want(total), kvh = total ? u / total : 0, p = u - kvh * total;
   if (p >= at && p < at + own) {
     int r = r0;
@@ -682,8 +689,8 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
     for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w][lane & 31][0]);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float mw = ml[w][lane & 31][0];
-      L += mw == kLowest ? 0.0f : ml[w][lane & 31][1] * exp2_fast((mw - M) * a.c);
+      const float mw = ml[w][lane & 31][0], lw = ml[w][lane & 31][1];
+      L += lw == 0.0f ? 0.0f : lw * exp2_fast((mw - M) * a.c);
     }
     const float f = rb.m == kLowest ? 0.0f : exp2_fast((rb.m - M) * a.c);
     float* so = (float*)(smem + wave * FK::kWave) + (lane & 31) * FK::kPitch;
@@ -718,7 +725,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
             u32x4{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv), T::pack(y[0] * inv, y[1] * inv),
                   T::pack(y[2] * inv, y[3] * inv)};
         if (a.lse && col == 0)
-          a.lse[(int64_t)(s.start + token) * a.HQ + head] = m == kLowest ? -INFINITY : m * a.scale + __logf(lr);
+          a.lse[(int64_t)(s.start + token) * a.HQ + head] = log_sum(a, m, lr);
       } else {
         const int64_t at = (int64_t)slot * kFewRows + rr;
         *(f32x4*)(a.few_part + at * DV + col) = x;
@@ -801,7 +808,7 @@ __global__ __launch_bounds__(256) void few_join_kernel(AttnArgs a) {
       for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
       const float next = fmaxf(M, top), f0 = M == kLowest ? 0.0f : exp2_fast((M - next) * a.c);
       const float f = mi == kLowest ? 0.0f : exp2_fast((mi - next) * a.c);
-      float sum = mi == kLowest ? 0.0f : f * li;
+      float sum = lane < n ? f * li : 0.0f;  // (NaN where a piece's scores are)
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
       L = L * f0 + sum;
@@ -834,7 +841,7 @@ __global__ __launch_bounds__(256) void few_join_kernel(AttnArgs a) {
     else
       *(uint16_t*)(out + lane * 2) = (uint16_t)u;
     if (a.lse && lane == 0)
-      a.lse[(int64_t)(rec.start + token) * a.HQ + head] = M == kLowest ? -INFINITY : M * a.scale + __logf(L);
+      a.lse[(int64_t)(rec.start + token) * a.HQ + head] = log_sum(a, M, L);
   }
 }
 

@@ -21,21 +21,6 @@ constexpr int kMaxThreads = 1024;
 constexpr int kTokensPerGroup = 2048;
 constexpr int kMostLen = 1 << 30;  // longer lengths count as this
 
-// Sums of non-negative numbers that stop at 2^31 - 1 (and so stay monotone)
-__device__ __forceinline__ int add_sat(int a, int b) { return __builtin_elementwise_add_sat(a, b); }
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ int add_dpp(int v) {
-  return add_sat(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, false));
-}
-__device__ __forceinline__ int wave_incl_sat(int v) {
-  v = add_dpp<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
-  v = add_dpp<0x112, 0xF>(v);
-  v = add_dpp<0x114, 0xF>(v);
-  v = add_dpp<0x118, 0xF>(v);
-  v = add_dpp<0x142, 0xA>(v);  // row_bcast 15, 31
-  return add_dpp<0x143, 0xC>(v);
-}
-
 // last i of n with v[i] <= x (v ascending, v[0] <= x)
 __device__ __forceinline__ int bisect(const int* v, int n, int x) {
   int lo = 0;

@@ -240,6 +240,32 @@ def test_paged_nonfinite(att):
     _check_paged(att, s, new, kv, window=20)
 
 
+@pytest.mark.parametrize("new,kv", [([1], [9000]), ([40, 1], [3000, 2500]), ([1, 1], [130, 40])])
+def test_paged_nan_rows(att, new, kv):
+    """A query of NaN, and a request whose first keys are NaN, give NaN and not what
+    the other pieces of a cut row hold; the other kv head's rows stay as they are."""
+    s = _paged(16, new, kv, 4, 2, 64, 64, 64, BF, "hnd", att)
+    clean, _ = _check_paged(att, s, new, kv)
+    s["q"][0, 1] = math.nan
+    _check_paged(att, s, new, kv)
+    s["q"][0, 1] = 1
+    for pos in range(min(kv[0], 600)):
+        s["ks"][0][pos, 0] = math.nan
+        s["kc"][int(s["table"][0, pos // 64]), pos % 64, 0] = math.nan
+    o, _ = _check_paged(att, s, new, kv)
+    assert o[: new[0], :2].isnan().all() and torch.equal(o[: new[0], 2:], clean[: new[0], 2:])
+
+
+@pytest.mark.parametrize("dims", [(64, 64), (192, 128)])
+def test_prompt_nan_rows(att, dims):
+    n, (D, DV) = 200, dims
+    q, k, v = _randn(1, n, 2, D, dtype=BF), _randn(2, n, 1, D, dtype=BF), _randn(3, n, 1, DV, dtype=BF)
+    q[7, 1] = math.nan
+    q[150, 0] = math.nan
+    k[190] = math.nan
+    _check_prompt(att, q, k, v, [n])
+
+
 def test_paged_matches_prompt(att):
     """A prompt's attention through the cache, whole and in chunks, is the packed kernel's."""
     n, HQ, HK, D = 230, 8, 2, 128
