@@ -319,6 +319,15 @@ struct TileKernel {
   }
 };
 
+// softmax(scale q k^T) v, one pass over the keys with the rows' running maximum
+// and sum, 128 rows (a token's g heads side by side) a workgroup.  64 KB of LDS
+// let two workgroups share a compute unit, so that one's exponentials run beside
+// the other's matrix instructions; these two, in about equal parts, are what
+// bounds it.  64 heads of 8192 tokens, causal: 1.00 ms, 1.10 PFLOP/s; 128 heads of
+// 192 (values 128), 2048 tokens: 199 us, 865 TFLOP/s; 56 heads, nine prompts of
+// 5003 tokens in all, window 1500: 86 us, 604 TFLOP/s (tiles at the window's two
+// edges are masked and count half).
+//
 // Grid: (kv heads) x (tile slots).  Sequence s has the slots from
 // floor(cu[s] g / BM) + s on: as many as its tiles, or one more, whatever the
 // lengths, so the grid follows from the totals alone.
@@ -544,7 +553,9 @@ __device__ __forceinline__ f32x2v* tile_ml(const AttnArgs& a, int at) {
   return (f32x2v*)a.tile_ml + (int64_t)at * 32 + (threadIdx.x & 31);
 }
 
-// requests of more than 32 rows
+// Requests of more than 32 rows: the prompt kernel's loop over pages.  Bound as
+// that one is, and by the pieces' sums (written and read once more).  Chunks of
+// four prompts (about 450 tokens of 56 heads each over up to 8700 keys): 331 us.
 template <typename T, int D, int DV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
   typedef TileKernel<T, D, DV, NW, true> TK;
@@ -584,7 +595,12 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
 
 // Requests of at most 32 rows (single tokens above all): the waves take 32 keys
 // each of a tile of 32 NW, through two LDS stages of their own, and join their
-// sums at the end of a piece.
+// sums at the end of a piece.  Bound by memory: nearly all of the LDS holds loads in
+// flight.  128 requests over 3.94 GB of cache 603 us (6.5 TB/s; a streaming read
+// reaches 6.95), 48 over 727 MB 116 us, one over 134 MB 28 us (ramp and the uneven
+// end of 8 or 9 tiles a workgroup).  Runs cut at 32 keys instead of 128 are more
+// even but slower (48 requests' calls 122 to 128 us, 100 over 1500 keys 67 to 74):
+// the waves of a workgroup then end at different times.
 template <typename T, int D, int DV, int NW>
 struct FewKernel {
   static constexpr int BN = 32 * NW;
@@ -744,7 +760,8 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
 __device__ __forceinline__ int piece_slot(int w, int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); }
 
 // Adds up the pieces of cut segments: of tiled rows, one workgroup a segment,
-// each wave its 32 rows, in the registers' order.
+// each wave its 32 rows, in the registers' order.  Bound by memory (up to 134 MB of
+// sums): 15 us beside the chunks of four prompts.
 template <typename T, int DV, int NW>
 __global__ __launch_bounds__(64 * NW) void tile_join_kernel(AttnArgs a) {
   const int w = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -785,7 +802,9 @@ __global__ __launch_bounds__(64 * NW) void tile_join_kernel(AttnArgs a) {
   store_out<T, DV>(a, o, M, L, s, r, rec.kvh);
 }
 
-// Of single rows: workgroup (w, y), one wave a row, DV / 64 columns a lane.
+// Of single rows: workgroup (w, y), one wave a row, DV / 64 columns a lane.  Bound
+// by its launch and two dependent reads: 5 us.  (16 pieces in flight instead of 8:
+// 32 of them 0.5 us faster, 4 of them 0.5 us slower.)
 template <typename T, int DV>
 __global__ __launch_bounds__(256) void few_join_kernel(AttnArgs a) {
   constexpr int NC = DV / 64;
