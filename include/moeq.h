@@ -521,7 +521,8 @@ moeq_status moeq_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int32
                          int32_t* kv_lens, int32_t* slots, int32_t* positions, void* stream);
 
 /* Stores token t's keys and values in slot slots[t]; slots outside the cache
- * (-1) are skipped.  Distinct tokens' slots must differ.
+ * (-1) are skipped.  Distinct tokens' slots must differ, and so must the cache's
+ * rows (no stride between two of them below their dim).
  *   head, n_kv_heads, head_dim, value_dim, dtype of `a` are used; any dims that
  *   are multiples of 8 up to 1024 serve here
  *   k, v    DEVICE [n_tokens x n_kv_heads x head_dim / value_dim]

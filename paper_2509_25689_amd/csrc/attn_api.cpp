@@ -106,6 +106,18 @@ moeq_status check_cache(const moeq_kv_cache* c) {
   return MOEQ_OK;
 }
 
+// a cache that is written: no two places, heads or pages at the same address
+moeq_status check_apart(const moeq_kv_cache* c, const moeq_attn* a) {
+  auto apart = [&](int64_t page, int64_t slot, int64_t head, int32_t dim) {
+    return slot >= dim && (a->n_kv_heads == 1 || head >= dim) && (c->n_pages == 1 || page >= dim);
+  };
+  if (!apart(c->k_page_stride, c->k_slot_stride, c->k_head_stride, a->head_dim) ||
+      !apart(c->v_page_stride, c->v_slot_stride, c->v_head_stride, a->value_dim))
+    return fail(MOEQ_ERR_INVALID_ARG, "the cache's rows overlap: a stride is below head_dim %d or value_dim %d",
+                a->head_dim, a->value_dim);
+  return MOEQ_OK;
+}
+
 void set_heads(AttnArgs& g, const moeq_attn* a) {
   g.HQ = a->n_heads;
   g.HK = a->n_kv_heads;
@@ -163,7 +175,7 @@ moeq_status moeq_kv_append(const moeq_attn* a, const moeq_kv_cache* cache, const
   if (a->head_dim % 8 || a->value_dim % 8 || a->head_dim > 1024 || a->value_dim > 1024)
     return fail(MOEQ_ERR_INVALID_ARG, "head_dim %d and value_dim %d must be multiples of 8 up to 1024", a->head_dim,
                 a->value_dim);
-  if ((st = check_cache(cache)) != MOEQ_OK) return st;
+  if ((st = check_cache(cache)) != MOEQ_OK || (st = check_apart(cache, a)) != MOEQ_OK) return st;
   if (n_tokens < 0 || n_tokens > kMaxRows)
     return fail(MOEQ_ERR_INVALID_ARG, "n_tokens %d must lie in 0 .. 2^24", n_tokens);
   if (n_tokens == 0) return MOEQ_OK;

@@ -96,3 +96,12 @@ def test_append_arguments():
     assert call(c=_cache(page_size=5)) == BAD and call(k=_rows(p=None)) == BAD and call(v=_rows(t=3)) == BAD
     assert call(slots=None) == BAD and call(T=-1) == BAD
     assert call(T=0) == moeq.MOEQ_OK
+
+
+@pytest.mark.parametrize("kw", [dict(k_page_stride=0), dict(k_slot_stride=64), dict(v_head_stride=0), dict(v_slot_stride=0)])
+def test_append_refuses_overlapping_rows(kw):
+    """Rows of a cache that share memory can be read, not written."""
+    assert L.moeq_kv_append(_attn(), _cache(**kw), _rows(), _rows(), FAKE, 4, None) == BAD
+    assert "overlap" in moeq.moeq_last_error()
+    one = _cache(n_pages=1, k_page_stride=0, v_page_stride=0)
+    assert L.moeq_kv_append(_attn(), one, _rows(), _rows(), FAKE, 0, None) == moeq.MOEQ_OK
