@@ -323,9 +323,9 @@ struct TileKernel {
 // and sum, 128 rows (a token's g heads side by side) a workgroup.  64 KB of LDS
 // let two workgroups share a compute unit, so that one's exponentials run beside
 // the other's matrix instructions; these two, in about equal parts, are what
-// bounds it.  64 heads of 8192 tokens, causal: 1.00 ms, 1.10 PFLOP/s; 128 heads of
-// 192 (values 128), 2048 tokens: 199 us, 865 TFLOP/s; 56 heads, nine prompts of
-// 5003 tokens in all, window 1500: 86 us, 604 TFLOP/s (tiles at the window's two
+// bounds it.  64 heads of 8192 tokens, causal: 0.96 ms, 1.14 PFLOP/s; 128 heads of
+// 192 (values 128), 2048 tokens: 193 us, 891 TFLOP/s; 56 heads, nine prompts of
+// 5003 tokens in all, window 1500: 87 us, 600 TFLOP/s (tiles at the window's two
 // edges are masked and count half).
 //
 // Grid: (kv heads) x (tile slots).  Sequence s has the slots from

@@ -209,10 +209,22 @@ struct RowBlock {
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+    // The fragments are read two steps ahead.  Left to the compiler, the kernels with
+    // full register files read each into the same registers and waited for it:
+    // chunks of four prompts 386 to 381 us a call, 8192 tokens 1003 to 994, 8
+    // requests of 192-wide heads 29.4 to 28.7 (one step ahead: the same, but short
+    // prompts 3 % slower).
+    u32x4 x = lds_read16(kt + a.k[0]), next = lds_read16(kt + a.k[1]);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // LDS reads
 #pragma unroll
     for (int t = 0; t < KS; ++t) {
-      s = T::mma(lds_read16(kt + a.k[t]), q[t], s);
+      const u32x4 y = lds_read16(kt + a.k[t + 2 < KS ? t + 2 : t]);
+      s = T::mma(x, q[t], s);
+      if (t + 2 < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
       between(t);
+      x = next;
+      next = y;
     }
     return s;
   }
