@@ -555,7 +555,7 @@ __device__ __forceinline__ f32x2v* tile_ml(const AttnArgs& a, int at) {
 
 // Requests of more than 32 rows: the prompt kernel's loop over pages.  Bound as
 // that one is, and by the pieces' sums (written and read once more).  Chunks of
-// four prompts (about 450 tokens of 56 heads each over up to 8700 keys): 331 us.
+// four prompts (about 450 tokens of 56 heads each over up to 8700 keys): 314 us.
 template <typename T, int D, int DV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
   typedef TileKernel<T, D, DV, NW, true> TK;
@@ -596,8 +596,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
 // Requests of at most 32 rows (single tokens above all): the waves take 32 keys
 // each of a tile of 32 NW, through two LDS stages of their own, and join their
 // sums at the end of a piece.  Bound by memory: nearly all of the LDS holds loads in
-// flight.  128 requests over 3.94 GB of cache 603 us (6.5 TB/s; a streaming read
-// reaches 6.95), 48 over 727 MB 116 us, one over 134 MB 28 us (ramp and the uneven
+// flight.  128 requests over 3.94 GB of cache 606 us (6.5 TB/s; a streaming read
+// reaches 6.95), 48 over 727 MB 115 us, one over 134 MB 26 us (ramp and the uneven
 // end of 8 or 9 tiles a workgroup).  Runs cut at 32 keys instead of 128 are more
 // even but slower (48 requests' calls 122 to 128 us, 100 over 1500 keys 67 to 74):
 // the waves of a workgroup then end at different times.
@@ -893,10 +893,15 @@ hipError_t launch_attn_prompt(AttnArgs a, int dtype, int D, hipStream_t s) {
     a.n_slots = (int)slots;
     // Heads in turn leave an XCD's 64 places (two a compute unit) uneven at the
     // end: the last ones' longest tile starts when the others are nearly done.
-    // So many at once that they give each place at least that tile's work (of
-    // slots (slots + 1) / 2 a head): 128 heads of 2048 tokens in 219 us, one
-    // after the other in 238, all 16 of an XCD together (its L2 misses) in 225.
-    a.heads_together = (int)std::max<long long>(1, std::min<long long>(a.HK / 8, (2 * 64 + slots) / (slots + 1)));
+    // So many at once that they give each place at least twice that tile's work (of
+    // slots (slots + 1) / 2 a head), and as many in the last group as in the others.
+    // 128 heads of 192 over 2048 tokens: 16 heads an XCD 8 at once 198 us, one after
+    // the other 206, all 16 (its L2 misses) 202; 64 heads over 4001 tokens 8 at once
+    // 277, 4 at once 283; 32 over four prompts of 5000 tokens in all, 4 at once 125,
+    // 3 and then 1 147.
+    const long long heads = std::max(1, a.HK / 8), most = std::min<long long>(heads, (4 * 64 + slots) / (slots + 1));
+    const long long groups = (heads + std::max(1LL, most) - 1) / std::max(1LL, most);
+    a.heads_together = (int)((heads + groups - 1) / groups);
     kernel<<<(unsigned)(slots * a.HK), 64 * NW, TK::lds, s>>>(a);
     return hipGetLastError();
   });

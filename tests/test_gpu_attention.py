@@ -75,6 +75,16 @@ def test_prompt_many_sequences(att):
     _check_prompt(att, q, k, v, lens)
 
 
+def test_prompt_many_heads(att):
+    """Heads that an XCD takes in groups of unequal size give what they give by eights."""
+    n, H = 9000, 40
+    q, k, v = (_randn(i, n, H, 64, dtype=BF) for i in (1, 2, 3))
+    cu = torch.tensor([0, n], dtype=torch.int32).cuda()
+    whole = att.prompt(q, k, v, cu)
+    for h in range(0, H, 8):
+        assert torch.equal(whole[:, h: h + 8], att.prompt(q[:, h: h + 8], k[:, h: h + 8], v[:, h: h + 8], cu)), h
+
+
 def test_prompt_strides(att):
     """Slices of a fused projection, head-major tensors, an output inside a larger one."""
     n, HQ, HK, D = 90, 6, 2, 128
