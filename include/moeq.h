@@ -521,8 +521,9 @@ moeq_status moeq_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int32
                          int32_t* kv_lens, int32_t* slots, int32_t* positions, void* stream);
 
 /* Stores token t's keys and values in slot slots[t]; slots outside the cache
- * (-1) are skipped.  Distinct tokens' slots must differ, and so must the cache's
- * rows (no stride between two of them below their dim).
+ * (-1) are skipped.  Distinct tokens' slots must differ, and the cache's rows must
+ * lie apart: taking pages, places and heads by stride, each stride is at least what
+ * those below it reach (as in slices and permutations of dense arrays).
  *   head, n_kv_heads, head_dim, value_dim, dtype of `a` are used; any dims that
  *   are multiples of 8 up to 1024 serve here
  *   k, v    DEVICE [n_tokens x n_kv_heads x head_dim / value_dim]
@@ -536,7 +537,7 @@ moeq_status moeq_kv_append(const moeq_attn* a, const moeq_kv_cache* cache, const
  *   q, k, v   DEVICE rows [n_tokens x heads x dims]
  *   cu        DEVICE int32 [n_seqs + 1], ascending, within 0 .. n_tokens
  *   out       DEVICE rows [n_tokens x n_heads x value_dim] (written), apart from
- *             each other and from q, k and v
+ *             each other (as the cache's rows for moeq_kv_append) and from q, k and v
  *   lse       DEVICE float [n_tokens x n_heads] (written): natural logarithm of
  *             each row's sum of exponentials; or NULL
  * Tokens of no sequence are not written.

@@ -3,6 +3,8 @@
 #include <math.h>
 #include <stdarg.h>
 
+#include <algorithm>
+
 #include "attention.h"
 
 using namespace moeq;
@@ -76,11 +78,29 @@ moeq_status check_rows(const moeq_rows* r, const char* name, bool neighbours) {
   return MOEQ_OK;
 }
 
-// rows that are written: no two at the same place
+// Rows of `dim` elements that are written must not meet.  Dimensions of more than one
+// element, by stride: each steps over all that those below it reach, as the
+// slices and permutations of a dense array do.
+struct Dim {
+  int64_t extent, stride;
+};
+template <int N>
+bool rows_apart(Dim (&d)[N], int64_t dim) {
+  std::sort(d, d + N, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  __int128 reach = dim;  // (extents to 2^27 times strides to 2^40)
+  for (const Dim& x : d) {
+    if (x.extent <= 1) continue;
+    if (x.stride < reach) return false;
+    reach += (__int128)(x.extent - 1) * x.stride;
+  }
+  return true;
+}
+
 moeq_status check_out(const moeq_rows* r, int64_t tokens, const moeq_attn* a) {
   const moeq_status st = check_rows(r, "out", false);
   if (st != MOEQ_OK) return st;
-  if ((tokens > 1 && r->token_stride < a->value_dim) || (a->n_heads > 1 && r->head_stride < a->value_dim))
+  Dim d[] = {{tokens, r->token_stride}, {a->n_heads, r->head_stride}};
+  if (!rows_apart(d, a->value_dim))
     return fail(MOEQ_ERR_INVALID_ARG, "out: rows %lld and %lld elements apart overlap", (long long)r->token_stride,
                 (long long)r->head_stride);
   return MOEQ_OK;
@@ -106,15 +126,14 @@ moeq_status check_cache(const moeq_kv_cache* c) {
   return MOEQ_OK;
 }
 
-// a cache that is written: no two places, heads or pages at the same address
+// a cache that is written
 moeq_status check_apart(const moeq_kv_cache* c, const moeq_attn* a) {
-  auto apart = [&](int64_t page, int64_t slot, int64_t head, int32_t dim) {
-    return slot >= dim && (a->n_kv_heads == 1 || head >= dim) && (c->n_pages == 1 || page >= dim);
-  };
-  if (!apart(c->k_page_stride, c->k_slot_stride, c->k_head_stride, a->head_dim) ||
-      !apart(c->v_page_stride, c->v_slot_stride, c->v_head_stride, a->value_dim))
-    return fail(MOEQ_ERR_INVALID_ARG, "the cache's rows overlap: a stride is below head_dim %d or value_dim %d",
-                a->head_dim, a->value_dim);
+  Dim k[] = {{c->n_pages, c->k_page_stride}, {c->page_size, c->k_slot_stride}, {a->n_kv_heads, c->k_head_stride}};
+  Dim v[] = {{c->n_pages, c->v_page_stride}, {c->page_size, c->v_slot_stride}, {a->n_kv_heads, c->v_head_stride}};
+  if (!rows_apart(k, a->head_dim) || !rows_apart(v, a->value_dim))
+    return fail(MOEQ_ERR_INVALID_ARG, "the cache's rows overlap: %lld, %lld and %lld (keys) or %lld, %lld and %lld (values) apart",
+                (long long)c->k_page_stride, (long long)c->k_slot_stride, (long long)c->k_head_stride,
+                (long long)c->v_page_stride, (long long)c->v_slot_stride, (long long)c->v_head_stride);
   return MOEQ_OK;
 }
 

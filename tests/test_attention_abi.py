@@ -105,3 +105,39 @@ def test_append_refuses_overlapping_rows(kw):
     assert "overlap" in moeq.moeq_last_error()
     one = _cache(n_pages=1, k_page_stride=0, v_page_stride=0)
     assert L.moeq_kv_append(_attn(), one, _rows(), _rows(), FAKE, 0, None) == moeq.MOEQ_OK
+
+
+def _nested(p, s, h):
+    return dict(k_page_stride=p, k_slot_stride=s, k_head_stride=h, v_page_stride=p, v_slot_stride=s, v_head_stride=h)
+
+
+@pytest.mark.parametrize("p,s,h", [(128, 128, 128),          # every stride one row
+                                   (8192, 128, 128),         # a place's heads on the next places
+                                   (16384, 128, 4096),       # the second head inside the first one's places
+                                   (8192, 256, 128),         # a page reaches into the next one
+                                   (256, 2048, 128)])        # so does a place, its pages side by side
+def test_append_refuses_rows_that_meet(p, s, h):
+    """Strides that each leave room for one row, and still lead two rows of a cache
+    (10 pages of 64 places, 2 heads of 128) to the same place."""
+    for which in ("k", "v"):
+        c = _cache(**{n: v for n, v in _nested(p, s, h).items() if n[0] == which})
+        assert L.moeq_kv_append(_attn(), c, _rows(), _rows(), FAKE, 0, None) == BAD, which
+        assert "overlap" in moeq.moeq_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(_nested(16384, 128, 8192)),                              # heads, places
+                                dict(_nested(16384, 256, 128)),                               # places, heads
+                                dict(_nested(256, 2560, 128)),                                # pages side by side
+                                dict(_nested(128, 2560, 1280)),                               # pages, heads, places
+                                dict(_nested(40000, 136, 9000)),                              # gaps everywhere
+                                dict(n_pages=1, **_nested(0, 256, 128)),
+                                dict(_nested(1 << 39, 1 << 20, 1 << 30))])                    # reaches past 64 bits' comfort
+def test_append_takes_rows_apart(kw):
+    assert L.moeq_kv_append(_attn(), _cache(**kw), _rows(), _rows(), FAKE, 0, None) == moeq.MOEQ_OK
+
+
+@pytest.mark.parametrize("t,h", [(128, 128), (512, 128), (128, 512), (1024, 1024), (136, 136)])
+def test_out_refuses_rows_that_meet(t, h):
+    """8 tokens of 8 heads of 128: each stride leaves room for a row, both together do not."""
+    assert _prompt(out=_rows(t=t, h=h)) == BAD and "overlap" in moeq.moeq_last_error()
+    assert _paged(out=_rows(t=t, h=h), tokens=8) == BAD and "overlap" in moeq.moeq_last_error()
