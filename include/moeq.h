@@ -505,7 +505,8 @@ typedef struct {
  *   block_table  DEVICE int32 [n_requests x max_blocks], rows table_stride
  *                apart; the entries of pages taken are written
  *   free_pages   DEVICE int32 [n_pages], the ring; pages given back are written
- *   pool_in      DEVICE int32 [3]: head (0 .. n_pages - 1), pages free, ignored
+ *   pool_in      DEVICE int32 [3]: head (modulo n_pages, of negative numbers too),
+ *                pages free, ignored
  *   pool_out     DEVICE int32 [3] (written; may be pool_in): head, pages free,
  *                requests refused
  *   n_tokens     the sum of the positive new_lens; tokens beyond it are dropped

@@ -51,7 +51,9 @@ __global__ __launch_bounds__(NT) void plan_kernel(PlanArgs a, bool fill, bool po
   constexpr int NW = NT / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t N = a.n_pages;
-  const uint32_t head_in = (uint32_t)a.pool_in[0], head = head_in < N ? head_in : head_in % N;
+  const int head_in = a.pool_in[0];
+  uint32_t head = (uint32_t)head_in;  // outside the ring: the place it comes to going round, before 0 as well
+  if (head >= N) head = head_in >= 0 ? head % N : N - 1 - (uint32_t)(-1 - head_in) % N;
   const int free0 = min(max(a.pool_in[1], 0), a.n_pages), room = a.n_pages - free0;
   const int P = 1 << a.page_shift;
   const bool first = blockIdx.x == 0;

@@ -188,3 +188,22 @@ def test_refusals(att):
         att.plan(s, s[:2], _dev([[0], [0], [0]]), s, _dev([0, 3, 0]), page_size=16, n_tokens=1)
     with pytest.raises(moeq.MoeqError):
         att.plan(s, s, _dev([[0], [0], [0]]), s, _dev([0, 3, 0]), page_size=24, n_tokens=1)
+
+
+@pytest.mark.parametrize("N", [1, 3, 7, 13, 48])
+@pytest.mark.parametrize("turn", [-3, -1, 1, 2])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_plan_head_outside_the_ring(att, N, turn, in_place):
+    """A head outside the ring is the place it comes to going round, before 0 as well."""
+    rng = random.Random(N * 10 + turn)
+    ids = list(range(N))
+    rng.shuffle(ids)
+    held = min(2, N - 1)
+    table = [ids[:held] + [-1] * (N + 1 - held), [-1] * (N + 1), [-1] * (N + 1)]
+    left = ids[held:]
+    head = rng.randrange(N)
+    free = [-1] * N
+    for i, b in enumerate(left):
+        free[(head + i) % N] = b
+    ctx, new = [16 * held, 0, 0], [-1 if held else 0, 17, 1]
+    _check(att, ctx, new, table, free, [head + turn * N, len(left), 0], 16, in_place=in_place)
