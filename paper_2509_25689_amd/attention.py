@@ -13,6 +13,9 @@ of a head together ("hnd") or all heads of a place ("nhd").  Work goes to
 Tensors made by an earlier call on another stream are the caller's to order, as
 everywhere in torch; those made here are kept for ``stream``.
 
+For inference: there is no backward, and a tensor that requires a gradient is
+refused while gradients are recorded.
+
 Wrong shapes, types, layouts and devices raise TypeError or ValueError, what the
 library refuses ``moeq.MoeqError``.
 """

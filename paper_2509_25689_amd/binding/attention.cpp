@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -43,7 +44,10 @@ struct PythonError {};
 
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) throw Raise{PyExc_TypeError, std::string(name) + " must be a torch tensor"};
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    refuse(name, "not require a gradient (there is no backward: use torch.no_grad() or detach())", t);
+  return t;
 }
 
 // The call's first tensor: on a GPU, the current one
@@ -309,7 +313,7 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return nullptr;
   }
   try {
-    const at::AutoDispatchBelowADInplaceOrView none;  // nothing here has a gradient
+    const at::AutoDispatchBelowADInplaceOrView none;  // nothing here has a gradient (tensor() sees to it)
     return F(args);
   } catch (const Raise& e) {
     PyErr_SetString(e.type, e.text.c_str());

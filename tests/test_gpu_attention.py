@@ -380,3 +380,31 @@ def test_refusals(att):
         att.paged(s["q"], s["kc"], s["vc"], s["cu"][:1], s["kv"], s["table"], max_new=1)
     # nothing to do is no error
     assert att.prompt(q[:0], k[:0], v[:0], torch.zeros(1, dtype=torch.int32).cuda()).shape == (0, 4, 128)
+
+
+def test_refuses_what_needs_a_gradient(att):
+    """There is no backward: an argument that a gradient would have to reach is refused, not cut off."""
+    n = 8
+    q, k, v = _randn(1, n, 4, 128, dtype=BF), _randn(2, n, 2, 128, dtype=BF), _randn(3, n, 2, 128, dtype=BF)
+    cu = torch.tensor([0, n], dtype=torch.int32).cuda()
+    s = _paged(15, [1], [40], 4, 2, 128, 128, 16, BF, "hnd", att)
+    ref = att.prompt(q, k, v, cu)
+    for i, name in enumerate("qkv"):
+        leaf = [t.clone() for t in (q, k, v)]
+        leaf[i].requires_grad_()
+        made = [t * 1 for t in leaf]                          # (not a leaf)
+        for args in (leaf, made):
+            with pytest.raises(ValueError, match=f"{name} .*gradient"):
+                att.prompt(*args, cu)
+            with torch.no_grad():
+                assert torch.equal(att.prompt(*args, cu), ref)
+            assert torch.equal(att.prompt(*(t.detach() for t in args), cu), ref)
+    for name in ("q", "kc", "vc"):
+        t = {**s, name: s[name].clone().requires_grad_()}
+        with pytest.raises(ValueError, match="gradient"):
+            att.paged(t["q"], t["kc"], t["vc"], t["cu"], t["kv"], t["table"], max_new=1)
+    side = torch.cuda.Stream()
+    with pytest.raises(ValueError, match="gradient"):
+        att.prompt(q.clone().requires_grad_(), k, v, cu, stream=side.cuda_stream)
+    with pytest.raises(ValueError, match="gradient"):
+        att.prompt(q, k, v, cu, out=torch.empty_like(q).requires_grad_())

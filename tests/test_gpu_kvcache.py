@@ -207,3 +207,17 @@ def test_plan_head_outside_the_ring(att, N, turn, in_place):
         free[(head + i) % N] = b
     ctx, new = [16 * held, 0, 0], [-1 if held else 0, 17, 1]
     _check(att, ctx, new, table, free, [head + turn * N, len(left), 0], 16, in_place=in_place)
+
+
+def test_refuses_what_needs_a_gradient(att):
+    """A cache write has no backward: what it would cut off is refused."""
+    kc, vc = att.empty_cache(4, 16, 2, 64)
+    k = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    grad = k.clone().requires_grad_()
+    s = _dev([0, 1, 2])
+    for name, args in (("k", (kc, vc, grad, k)), ("v", (kc, vc, k, grad * 2)), ("k_cache", (kc.clone().requires_grad_(), vc, k, k)),
+                       ("v_cache", (kc, vc.clone().requires_grad_(), k, k))):
+        with pytest.raises(ValueError, match=f"^{name} .*gradient"):
+            att.append(*args, s)
+        with torch.no_grad():
+            att.append(*args, s)
