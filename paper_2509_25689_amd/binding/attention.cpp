@@ -157,6 +157,12 @@ void done(moeq_status st) {
   if (st != MOEQ_OK) throw Failed{st};
 }
 
+// A tensor that the call has written: autograd, which may keep it, counts that.
+// (Inference tensors have no count.)
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // out, if given, else a new tensor
 at::Tensor output(PyObject* o, const char* name, at::ScalarType dtype, at::IntArrayRef shape, const at::Tensor& like) {
   if (o == Py_None) return at::empty(shape, like.options().dtype(dtype));
@@ -194,6 +200,9 @@ PyObject* plan(PyObject* const* a) {
                     narrow(width, "the table's width"), (int32_t*)free.data_ptr(), narrow(free.size(0), "the number of pages"),
                     pool, out, narrow(number(a[5]), "page_size"), narrow(T, "n_tokens"), cu, lens, slots, positions,
                     stream(a[9], ctx)));
+  written(table);
+  written(free);
+  if (a[7] != Py_None) written(tensor(a[7], "pool_out"));
   const std::vector<at::Tensor> parts = all.unsafe_split_with_sizes({R + 1, R, T, T, 3});
   PyObject* t = PyTuple_New(7);
   if (!t) throw PythonError{};
@@ -220,6 +229,8 @@ PyObject* append(PyObject* const* a) {
   const moeq_rows kr = rows(a[2], "k", dt, T, c.heads, c.dim, k), vr = rows(a[3], "v", dt, T, c.heads, c.value_dim, k);
   const moeq_attn d = describe(c.heads, c.heads, c.dim, c.value_dim, dt);
   done(moeq_kv_append(&d, &c.c, &kr, &vr, ints(a[4], "slots", T, k), narrow(T, "the number of tokens"), stream(a[5], k)));
+  written(tensor(a[0], "k_cache"));
+  written(tensor(a[1], "v_cache"));
   Py_RETURN_NONE;
 }
 
@@ -246,6 +257,7 @@ PyObject* prompt(PyObject* const* a) {
   done(moeq_attn_prompt(&d, &qr, &kr, &vr, cp, narrow(cu.size(0) - 1, "the number of sequences"),
                         narrow(T, "the number of tokens"), &orow, with ? (float*)lse.data_ptr() : nullptr,
                         stream(a[9], q)));
+  written(out);
   return with ? pair(out, lse) : THPVariable_Wrap(out);
 }
 
@@ -283,6 +295,7 @@ PyObject* paged(PyObject* const* a) {
                        narrow(width, "the table's width"), narrow(R, "the number of requests"),
                        narrow(T, "the number of tokens"), max_new, &orow, with ? (float*)lse.data_ptr() : nullptr,
                        ws.data_ptr(), (uint64_t)ws.numel(), stream(a[13], q)));
+  written(out);
   return with ? pair(out, lse) : THPVariable_Wrap(out);
 }
 

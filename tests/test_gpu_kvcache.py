@@ -221,3 +221,43 @@ def test_refuses_what_needs_a_gradient(att):
             att.append(*args, s)
         with torch.no_grad():
             att.append(*args, s)
+
+
+def test_writes_are_counted(att):
+    """What a call writes in place has a new version, which is how autograd notices
+    that a tensor it keeps for a backward was overwritten; inference tensors have none."""
+    kc, vc = att.empty_cache(4, 16, 2, 64)
+    k = torch.randn((3, 2, 64), device="cuda").bfloat16()
+    x = torch.ones((2, 64), device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    kc.zero_()
+    y = (x * kc[0, 0]).sum()
+    before = [t._version for t in (kc, vc)]
+    att.append(kc, vc, k, k, _dev([0, 1, 2]))
+    assert [t._version for t in (kc, vc)] == [n + 1 for n in before]
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
+    args = [_dev([0, 5]), _dev([3, -1]), _dev([[-1, -1], [2, -1]]), _dev([0, 1, 3, -1]), _dev([0, 3, 0])]
+    before = [t._version for t in args]
+    att.plan(*args, page_size=16, n_tokens=3)
+    assert [t._version - n for t, n in zip(args, before)] == [0, 0, 1, 1, 0]
+    att.plan(*args, page_size=16, n_tokens=3, pool_out=args[4])
+    assert [t._version - n for t, n in zip(args, before)] == [0, 0, 2, 2, 1]
+    with torch.inference_mode():
+        cache = att.empty_cache(4, 16, 2, 64)
+        att.append(*cache, k, k, _dev([0, 1, 2]))
+    att.append(*cache, k, k, _dev([3, 4, 5]))
+    assert torch.equal(cache[0][0, 3:6], k)
+
+
+def test_outputs_written_are_counted(att):
+    n = 8
+    q, k = torch.randn((n, 4, 64), device="cuda").bfloat16(), torch.randn((n, 2, 64), device="cuda").bfloat16()
+    kc, vc = att.empty_cache(2, 16, 2, 64)
+    att.append(kc, vc, k, k, torch.arange(n, device="cuda").int())
+    before = [t._version for t in (q, k, kc, vc)]
+    for call in (lambda out: att.prompt(q, k, k, _dev([0, n]), out=out),
+                 lambda out: att.paged(q, kc, vc, _dev([0, n]), _dev([n]), _dev([[0]]), max_new=n, out=out)):
+        out = torch.zeros_like(q)
+        was = out._version
+        assert call(out).data_ptr() == out.data_ptr() and out._version == was + 1
+    assert [t._version for t in (q, k, kc, vc)] == before
