@@ -458,7 +458,8 @@ enum { MOEQ_BF16 = 0, MOEQ_F16 = 1 };
  *   scale       factor of the scores, finite and positive
  * A row that sees no key has output 0 and lse -infinity.  Scores, softmax
  * statistics and sums are float32; the weights are rounded once to dtype
- * before they multiply the values, the output once. */
+ * before they multiply the values, the output once.  (Weights below 2^-32 of a
+ * row's largest may count as 0 in MOEQ_F16.) */
 typedef struct {
   int32_t n_heads;
   int32_t n_kv_heads;

@@ -141,8 +141,10 @@ __device__ __forceinline__ const char* q_row(const AttnArgs& a, const Seq& s, co
 
 // A row without keys has m = kLowest and l = 0.  (Scores that are all NaN leave m
 // there too, but l is NaN: where rows' parts are joined, l says whether there is one.)
+template <typename T>
 __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
-  return l == 0.0f ? -INFINITY : m * a.scale + __logf(l);
+  constexpr float ln2 = 0.69314718055994531f;
+  return l == 0.0f ? -INFINITY : m * a.scale + (__logf(l) - T::kLift * ln2);
 }
 
 template <typename T, int DV, int DB>
@@ -169,7 +171,7 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const f32x16 (&o)[D
       if (r.valid) *(u32x4*)(row + (32 * b + 16 * t + 8 * h) * 2) = u32x4{u[0], w[0], u[1], w[1]};
     }
   if (a.lse && r.valid && h == 0)
-    a.lse[(int64_t)(s.start + r.token) * a.HQ + head] = log_sum(a, m, l);
+    a.lse[(int64_t)(s.start + r.token) * a.HQ + head] = log_sum<T>(a, m, l);
 }
 
 // The order in which the key tiles of [lo, hi) are taken, `width` keys each, the
@@ -741,7 +743,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
             u32x4{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv), T::pack(y[0] * inv, y[1] * inv),
                   T::pack(y[2] * inv, y[3] * inv)};
         if (a.lse && col == 0)
-          a.lse[(int64_t)(s.start + token) * a.HQ + head] = log_sum(a, m, lr);
+          a.lse[(int64_t)(s.start + token) * a.HQ + head] = log_sum<T>(a, m, lr);
       } else {
         const int64_t at = (int64_t)slot * kFewRows + rr;
         *(f32x4*)(a.few_part + at * DV + col) = x;
@@ -860,7 +862,7 @@ __global__ __launch_bounds__(256) void few_join_kernel(AttnArgs a) {
     else
       *(uint16_t*)(out + lane * 2) = (uint16_t)u;
     if (a.lse && lane == 0)
-      a.lse[(int64_t)(rec.start + token) * a.HQ + head] = log_sum(a, M, L);
+      a.lse[(int64_t)(rec.start + token) * a.HQ + head] = log_sum<T>(a, M, L);
   }
 }
 

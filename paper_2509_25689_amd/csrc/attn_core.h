@@ -29,8 +29,10 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 
-// low, high: a dword's two values
+// low, high: a dword's two values.  kLift: the largest weight of a row is held as
+// 2^kLift or more before it is rounded.
 struct Bf16 {
+  static constexpr float kLift = 0.0f;
   static __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
   static __device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
   static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
@@ -44,6 +46,12 @@ struct Bf16 {
 };
 
 struct F16 {
+  // Unlifted, weights below 2^-25 of the largest would be 0 in the product and not in
+  // the sum, and 30000 keys of such weights are 2^-10 of a row.  Lifted, they count
+  // down to 2^-32; with kSlack the largest is 2^15 at most, and this type ends at
+  // 2^16.  No time: 128 requests over 3.94 GB 617 us a call with and without, nine
+  // prompts of 5003 tokens in all 86.6.
+  static constexpr float kLift = 7.0f;
   static __device__ __forceinline__ float low(uint32_t v) { return (float)__builtin_bit_cast(f16x2, v)[0]; }
   static __device__ __forceinline__ float high(uint32_t v) { return (float)__builtin_bit_cast(f16x2, v)[1]; }
   static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
@@ -167,7 +175,7 @@ struct RowBlock {
   u32x4 q[KS];
   f32x16 o[DB];
   float m;      // the maximum that the exponents are taken against (raw scores), kLowest: no key yet
-  float neg_mc; // -m * c, 0 while there is no key
+  float neg_mc; // kLift - m * c, 0 while there is no key: a weight is exp2(s * c + neg_mc)
   float l;      // this lane's share of the row's sum (its half of the keys)
 
   __device__ __forceinline__ void clear() {
@@ -257,9 +265,9 @@ struct RowBlock {
   // t: the lane's largest new score
   __device__ __forceinline__ void rescale(float t, float c) {
     t = max_halves(t);
-    if (__any(fmaf(t, c, neg_mc) > kSlack || (m == kLowest && t > kLowest))) {
+    if (__any(fmaf(t, c, neg_mc) > kSlack + T::kLift || (m == kLowest && t > kLowest))) {
       const float mn = fmaxf(m, t);
-      const float nmc = mn == kLowest ? 0.0f : -mn * c;
+      const float nmc = mn == kLowest ? 0.0f : fmaf(-mn, c, T::kLift);
       const float f = m == kLowest ? 0.0f : exp2_fast(nmc - neg_mc);
 #pragma unroll
       for (int b = 0; b < DB; ++b)
