@@ -43,13 +43,16 @@ def _new(like, shape, dtype, stream):
     return t
 
 
-def _for_stream(q, value_dim, out, lse, stream):
-    """out and lse, made here where the call goes to a stream of its own."""
-    if isinstance(q, torch.Tensor) and q.is_cuda and q.dim() == 3:
-        if out is None:
-            out = _new(q, (*q.shape[:2], value_dim), q.dtype, stream)
-        if lse:
-            lse = _new(q, q.shape[:2], torch.float32, stream)
+def _is(t, dims):
+    return isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == dims
+
+
+def _for_stream(q, v, out, lse, stream):
+    """out and lse, made here where the call goes to a stream of its own (q and v are checked)."""
+    if out is None:
+        out = _new(q, (*q.shape[:2], v.shape[-1]), q.dtype, stream)
+    if lse:
+        lse = _new(q, q.shape[:2], torch.float32, stream)
     return out, lse
 
 
@@ -79,7 +82,7 @@ def plan(ctx_lens, new_lens, block_table, free_pages, pool, *, page_size, n_toke
     block_table, free_pages, pool_out [3]: head, pages free, requests refused).
     pool_out: a new tensor by default; may be `pool` itself."""
     buffer = None
-    if stream is not None and isinstance(ctx_lens, torch.Tensor) and ctx_lens.is_cuda and n_tokens >= 0:
+    if stream is not None and _is(ctx_lens, 1) and n_tokens >= 0:
         buffer = _new(ctx_lens, 2 * ctx_lens.numel() + 2 * n_tokens + 4, torch.int32, stream)
     return _c.plan(ctx_lens, new_lens, block_table, free_pages, pool, page_size, n_tokens, pool_out, buffer, stream)
 
@@ -96,8 +99,8 @@ def prompt(q, k, v, cu_seqlens, *, causal=True, window=0, scale=None, out=None, 
     -> out [T, heads, value dim], with return_lse also lse float32 [T, heads].
     scale: dim ** -0.5 by default."""
     lse = True if return_lse else None
-    if stream is not None:
-        out, lse = _for_stream(q, v.shape[-1], out, lse, stream)
+    if stream is not None and _is(q, 3) and _is(v, 3):
+        out, lse = _for_stream(q, v, out, lse, stream)
     return _c.prompt(q, k, v, cu_seqlens, causal, window, scale, out, lse, stream)
 
 
@@ -109,9 +112,9 @@ def paged(q, k_cache, v_cache, cu_q, kv_lens, block_table, *, max_new, causal=Tr
     float32 [T, heads].  max_new: at least the most new tokens of a request.
     workspace: a uint8 tensor of paged_workspace(..) bytes, else made here."""
     lse = True if return_lse else None
-    if stream is not None:
-        out, lse = _for_stream(q, v_cache.shape[-1], out, lse, stream)
-        if workspace is None and isinstance(q, torch.Tensor) and q.is_cuda and q.dim() == 3:
+    if stream is not None and _is(q, 3) and _is(k_cache, 4) and _is(v_cache, 4):
+        out, lse = _for_stream(q, v_cache, out, lse, stream)
+        if workspace is None:
             n = paged_workspace(q.shape[1], k_cache.shape[2], q.shape[2], v_cache.shape[-1], max_new=max_new)
             workspace = _new(q, n, torch.uint8, stream)
     return _c.paged(q, k_cache, v_cache, cu_q, kv_lens, block_table, max_new, causal, window, scale, out, lse, workspace, stream)

@@ -141,3 +141,19 @@ def test_out_refuses_rows_that_meet(t, h):
     """8 tokens of 8 heads of 128: each stride leaves room for a row, both together do not."""
     assert _prompt(out=_rows(t=t, h=h)) == BAD and "overlap" in moeq.moeq_last_error()
     assert _paged(out=_rows(t=t, h=h), tokens=8) == BAD and "overlap" in moeq.moeq_last_error()
+
+
+def test_python_refusals_on_a_stream_of_its_own():
+    """With `stream` given a wrong argument is refused as it is without."""
+    torch = pytest.importorskip("torch")
+    attention = pytest.importorskip("paper_2509_25689_amd.attention")
+    q, c = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((2, 16, 2, 64), dtype=torch.bfloat16)
+    cu, table = torch.tensor([0, 3], dtype=torch.int32), torch.zeros((1, 1), dtype=torch.int32)
+    for stream in (None, 0):
+        for v in (None, [1.0], torch.zeros(())):
+            with pytest.raises((TypeError, ValueError)):
+                attention.prompt(q, q, v, cu, stream=stream)
+            with pytest.raises((TypeError, ValueError)):
+                attention.paged(q, c, v, cu, cu[1:], table, max_new=3, stream=stream)
+            with pytest.raises((TypeError, ValueError)):
+                attention.paged(q, v, c, cu, cu[1:], table, max_new=3, stream=stream)

@@ -408,3 +408,29 @@ def test_refuses_what_needs_a_gradient(att):
         att.prompt(q.clone().requires_grad_(), k, v, cu, stream=side.cuda_stream)
     with pytest.raises(ValueError, match="gradient"):
         att.prompt(q, k, v, cu, out=torch.empty_like(q).requires_grad_())
+
+
+def test_refusals_on_a_stream_of_its_own(att):
+    """With `stream` given a wrong argument is refused as it is without, before anything is allocated for it."""
+    from paper_2509_25689_amd import moeq
+    q = _randn(1, 3, 4, 64, dtype=BF)
+    s = _paged(15, [1], [40], 4, 2, 64, 64, 16, BF, "hnd", att)
+    rest = (s["cu"], s["kv"], s["table"])
+    cu = torch.tensor([0, 3], dtype=torch.int32).cuda()
+    side = torch.cuda.Stream()
+    for stream in (None, side.cuda_stream):
+        for bad in (None, [1.0], torch.zeros((), device="cuda"), torch.zeros(3, dtype=BF, device="cuda")):
+            with pytest.raises((TypeError, ValueError)):
+                att.prompt(q, q, bad, cu, stream=stream)
+            with pytest.raises((TypeError, ValueError)):
+                att.paged(s["q"], bad, s["vc"], *rest, max_new=1, stream=stream)
+            with pytest.raises((TypeError, ValueError)):
+                att.paged(s["q"], s["kc"], bad, *rest, max_new=1, stream=stream)
+        with pytest.raises(ValueError):
+            att.paged(s["q"].long(), s["kc"].long(), s["vc"].long(), *rest, max_new=1, stream=stream)
+        with pytest.raises(moeq.MoeqError):
+            att.paged(s["q"], s["kc"], s["vc"], *rest, max_new=-1, stream=stream)
+        with pytest.raises((TypeError, ValueError)):
+            att.plan(cu, cu, s["table"], cu, cu, page_size=16, n_tokens=None, stream=stream)
+        with pytest.raises((TypeError, ValueError)):
+            att.plan(cu, cu, s["table"], cu, cu, page_size=16, n_tokens=-1, stream=stream)
