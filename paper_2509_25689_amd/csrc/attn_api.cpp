@@ -39,6 +39,7 @@ int log2_of(int p) {
 constexpr int kMaxHeads = 4096;
 constexpr int kMaxGroup = 256;
 constexpr int kMaxRows = 1 << 24;  // tokens of a call
+constexpr int64_t kMaxThreads = 0xFFFFFF00LL;  // of a launch: below 2^32, in whole workgroups of 256
 
 moeq_status check_heads(const moeq_attn* a) {
   if (!a) return fail(MOEQ_ERR_INVALID_ARG, "the attention's description is NULL");
@@ -200,7 +201,9 @@ moeq_status moeq_kv_append(const moeq_attn* a, const moeq_kv_cache* cache, const
   if (n_tokens == 0) return MOEQ_OK;
   if ((st = check_rows(k, "k", false)) != MOEQ_OK || (st = check_rows(v, "v", false)) != MOEQ_OK) return st;
   if (!slots || !aligned4(slots)) return fail(MOEQ_ERR_INVALID_ARG, "slots must be 4-byte aligned and not NULL");
-  if ((int64_t)n_tokens * a->n_kv_heads * 128 / 256 > 0x7FFFFFFFLL)
+  // (a thread copies one chunk, or four where there are many)
+  const int64_t chunks = std::max(a->head_dim, a->value_dim) / 8 * (int64_t)a->n_kv_heads;
+  if (chunks * ((n_tokens + 3) / 4) > kMaxThreads)
     return fail(MOEQ_ERR_UNSUPPORTED, "n_tokens %d of %d kv heads exceed a launch", n_tokens, a->n_kv_heads);
   AppendArgs g{};
   g.k = (const char*)k->p;
@@ -234,6 +237,9 @@ moeq_status moeq_attn_prompt(const moeq_attn* a, const moeq_rows* q, const moeq_
   if (st != MOEQ_OK) return st;
   if ((st = check_counts(a, n_seqs, n_tokens, "n_seqs")) != MOEQ_OK) return st;
   if (n_seqs == 0 || n_tokens == 0) return MOEQ_OK;
+  if ((int64_t)n_tokens * a->n_heads / 128 + (int64_t)n_seqs * a->n_kv_heads > kMaxThreads / 256)
+    return fail(MOEQ_ERR_UNSUPPORTED, "n_seqs %d, n_tokens %d and %d heads exceed a launch's workgroups", n_seqs, n_tokens,
+                a->n_heads);
   if ((st = check_rows(q, "q", false)) != MOEQ_OK || (st = check_rows(k, "k", true)) != MOEQ_OK ||
       (st = check_rows(v, "v", true)) != MOEQ_OK || (st = check_out(out, n_tokens, a)) != MOEQ_OK)
     return st;

@@ -157,3 +157,17 @@ def test_python_refusals_on_a_stream_of_its_own():
                 attention.paged(q, c, v, cu, cu[1:], table, max_new=3, stream=stream)
             with pytest.raises((TypeError, ValueError)):
                 attention.paged(q, v, c, cu, cu[1:], table, max_new=3, stream=stream)
+
+
+def test_more_workgroups_than_a_launch_has():
+    """A launch has fewer than 2^32 threads in a dimension; what needs more is refused as
+    unsupported, not by the device."""
+    mha = dict(n_heads=128, n_kv_heads=128)
+    assert _prompt(_attn(**mha), seqs=1 << 17, tokens=1 << 16, out=_rows(t=1 << 14)) == UNSUP and "workgroups" in moeq.moeq_last_error()
+    assert _prompt(_attn(n_heads=4096, n_kv_heads=16), seqs=1 << 20, tokens=1 << 10, out=_rows(t=1 << 19)) == UNSUP
+
+    def append(tokens, kv_heads, dim):
+        a = _attn(n_heads=kv_heads, n_kv_heads=kv_heads, head_dim=dim, value_dim=64)
+        c = _cache(**_nested(1 << 30, 1024, 1 << 17))
+        return L.moeq_kv_append(a, c, _rows(), _rows(), FAKE, tokens, None)
+    assert append(1 << 24, 64, 128) == UNSUP and append(1 << 24, 8, 1024) == UNSUP and append(1 << 24, 4096, 8) == UNSUP
