@@ -17,7 +17,7 @@ For inference: there is no backward, and a tensor that requires a gradient is
 refused while gradients are recorded.
 
 Wrong shapes, types, layouts and devices raise TypeError or ValueError, what the
-library refuses ``moeq.MoeqError``.
+library refuses ``moeq.MoeqError``, outputs that do not fit torch.OutOfMemoryError.
 """
 import torch
 
@@ -28,7 +28,7 @@ try:
 except ImportError as e:
     raise ImportError(f"the compiled binding of the attention operators does not load ({e}); run __graft_entry__.build()") from e
 
-_c.setup(moeq.MoeqError, torch._C._cuda_getCurrentRawStream)
+_c.setup(moeq.MoeqError, torch.OutOfMemoryError, torch._C._cuda_getCurrentRawStream)
 
 
 def _new(like, shape, dtype, stream):

@@ -5,7 +5,7 @@
 // Python, as does the step plan, 3.5 of them the launch.
 //
 // attention.py documents the functions; these take its arguments in order, and
-// raise TypeError, ValueError or MoeqError.
+// raise TypeError, ValueError, MoeqError or torch.OutOfMemoryError.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -22,6 +22,7 @@
 namespace {
 
 PyObject* g_error = nullptr;       // moeq.MoeqError
+PyObject* g_memory_error = nullptr;  // torch.OutOfMemoryError
 PyObject* g_raw_stream = nullptr;  // device index -> current stream as an integer
 
 struct Raise {
@@ -307,14 +308,14 @@ PyObject* paged_workspace(PyObject* const* a) {
   return PyLong_FromUnsignedLongLong(bytes);
 }
 
-// MoeqError, the function for the current stream
+// MoeqError, torch.OutOfMemoryError, the function for the current stream
 PyObject* setup(PyObject* const* a) {
-  Py_INCREF(a[0]);
-  Py_INCREF(a[1]);
-  Py_XDECREF(g_error);
-  Py_XDECREF(g_raw_stream);
-  g_error = a[0];
-  g_raw_stream = a[1];
+  PyObject** const to[] = {&g_error, &g_memory_error, &g_raw_stream};
+  for (int i = 0; i < 3; ++i) {
+    Py_INCREF(a[i]);
+    Py_XDECREF(*to[i]);
+    *to[i] = a[i];
+  }
   Py_RETURN_NONE;
 }
 
@@ -337,6 +338,8 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
       Py_DECREF(o);
     }
   } catch (const PythonError&) {
+  } catch (const c10::OutOfMemoryError& e) {
+    PyErr_SetString(g_memory_error, e.what_without_backtrace());
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   } catch (...) {
@@ -348,7 +351,7 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define MOEQ_METHOD(f, n) \
   { #f, (PyCFunction)(void (*)(void))call<f, n>, METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {MOEQ_METHOD(plan, 10),  MOEQ_METHOD(append, 6),          MOEQ_METHOD(prompt, 10),
-                         MOEQ_METHOD(paged, 14), MOEQ_METHOD(paged_workspace, 5), MOEQ_METHOD(setup, 2),
+                         MOEQ_METHOD(paged, 14), MOEQ_METHOD(paged_workspace, 5), MOEQ_METHOD(setup, 3),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attention", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -434,3 +434,19 @@ def test_refusals_on_a_stream_of_its_own(att):
             att.plan(cu, cu, s["table"], cu, cu, page_size=16, n_tokens=None, stream=stream)
         with pytest.raises((TypeError, ValueError)):
             att.plan(cu, cu, s["table"], cu, cu, page_size=16, n_tokens=-1, stream=stream)
+
+
+def test_out_of_memory(att):
+    """An output that does not fit is torch's own error for that, which a serving program catches."""
+    n, H = 1 << 16, 256
+    q, k = torch.zeros((1, 1, 128), dtype=BF, device="cuda").expand(n, H, 128), torch.zeros((1, 1, 128), dtype=BF, device="cuda").expand(n, 1, 128)
+    cu = torch.tensor([0, n], dtype=torch.int32).cuda()
+    torch.cuda.empty_cache()
+    torch.cuda.set_per_process_memory_fraction(0.01)           # 4 GB do not fit
+    try:
+        with pytest.raises(torch.cuda.OutOfMemoryError):
+            att.prompt(q, k, k, cu)
+        with pytest.raises(torch.cuda.OutOfMemoryError):
+            att.prompt(q, k, k, cu, stream=torch.cuda.Stream().cuda_stream)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
