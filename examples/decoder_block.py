@@ -122,15 +122,18 @@ def main(layer="tiny", requests=6, steps=12, chunk=48, verbose=True):
     """Serves `requests` prompts of different lengths, some of them in chunks, and
     `steps` tokens of each; returns the largest difference of an output from the
     same request run as one prompt, relative to the outputs' size."""
-    block = Block(layer, max_tokens=1024)
-    server = Server(block, places=4, n_pages=64, page_size=16, max_blocks=16)
+    places, page_size = 4, 16
+    lengths = [5 + 29 * i % 131 for i in range(requests)]
+    blocks = -(-(max(lengths, default=0) + steps) // page_size) + 1
+    block = Block(layer, max_tokens=max(1024, blocks * page_size))  # (the last pass takes a request's tokens as one prompt)
+    server = Server(block, places=places, n_pages=places * blocks, page_size=page_size, max_blocks=blocks)
     g = torch.Generator(device="cuda").manual_seed(2)
-    waiting = [(i, torch.randn((5 + 29 * i % 131, block.shape.hidden), generator=g, device="cuda").bfloat16()) for i in range(requests)]
+    waiting = [(i, torch.randn((n, block.shape.hidden), generator=g, device="cuda").bfloat16()) for i, n in enumerate(lengths)]
     running, history, outputs = {}, {}, {}  # place -> [request, rows left to add, tokens left]
     n_steps = n_tokens = 0
     done = []
     while waiting or running or done:
-        for r in range(4):
+        for r in range(places):
             if r not in running and r not in done and waiting:
                 i, x = waiting.pop(0)
                 running[r] = [i, x, steps]

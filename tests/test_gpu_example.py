@@ -22,3 +22,15 @@ def test_decoder_block(gpu_lib, chunk):
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
     assert m.main("tiny", requests=6, steps=8, chunk=chunk, verbose=False) < 8 * 2.0 ** -8
+
+
+def test_decoder_block_many_steps(gpu_lib):
+    """Requests that grow by far more than their prompts: the cache is sized for the
+    steps asked for.  Hundreds of tokens a request hold some whose router scores
+    nearly tie; a token that takes another expert differs by twice its output at most,
+    so one in 16 such tokens are 1/2 in the norm.  (Tokens served from wrong pages would be
+    unrelated to the prompt's: 2 ** 0.5.)"""
+    spec = importlib.util.spec_from_file_location("decoder_block", PATH)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    assert m.main("tiny", requests=5, steps=200, chunk=48, verbose=False) < 0.5
