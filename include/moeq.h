@@ -501,7 +501,9 @@ typedef struct {
  * (a ring of n_pages entries) and go back to its tail.  A request whose pages
  * do not fit max_blocks, or which needs pages and the pages needed up to and
  * with it exceed those free at the step's start, is refused: it takes none, its
- * slots are -1 and its kv_len 0; the others are served.
+ * slots are -1 and its kv_len 0.  (The pages that it needed still count, unless
+ * they did not fit max_blocks: once one request does not find its pages, the later
+ * ones that need any do not either.  Those that need none are served.)
  *   ctx_lens, new_lens  DEVICE int32 [n_requests], at most 2^30
  *   block_table  DEVICE int32 [n_requests x max_blocks], rows table_stride
  *                apart; the entries of pages taken are written
@@ -526,8 +528,8 @@ moeq_status moeq_kv_plan(const int32_t* ctx_lens, const int32_t* new_lens, int32
  * (-1) are skipped.  Distinct tokens' slots must differ, and the cache's rows must
  * lie apart: taking pages, places and heads by stride, each stride is at least what
  * those below it reach (as in slices and permutations of dense arrays).
- *   head, n_kv_heads, head_dim, value_dim, dtype of `a` are used; any dims that
- *   are multiples of 8 up to 1024 serve here
+ *   n_heads, n_kv_heads, head_dim, value_dim, dtype of `a` are checked; any dims
+ *   that are multiples of 8 up to 1024 serve here
  *   k, v    DEVICE [n_tokens x n_kv_heads x head_dim / value_dim]
  *   slots   DEVICE int32 [n_tokens]
  * Errors: INVALID_ARG, DEVICE. */

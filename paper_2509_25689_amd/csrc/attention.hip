@@ -325,10 +325,12 @@ struct TileKernel {
 // and sum, 128 rows (a token's g heads side by side) a workgroup.  64 KB of LDS
 // let two workgroups share a compute unit, so that one's exponentials run beside
 // the other's matrix instructions; these two, in about equal parts, are what
-// bounds it.  64 heads of 8192 tokens, causal: 0.96 ms, 1.14 PFLOP/s; 128 heads of
-// 192 (values 128), 2048 tokens: 193 us, 891 TFLOP/s; 56 heads, nine prompts of
-// 5003 tokens in all, window 1500: 87 us, 600 TFLOP/s (tiles at the window's two
-// edges are masked and count half).
+// bounds it (matrix units busy 59 % of the time, vector units 55 %).  64 heads of
+// 8192 tokens, causal: 1.00 ms, 1.10 PFLOP/s; 128 heads of 192 (values 128), 2048
+// tokens: 198 us, 868 TFLOP/s; 56 heads of 8192 tokens, the last 1500 of them seen:
+// 330 us, 971 TFLOP/s; 56 heads, nine prompts of 159 to 1099 tokens: 87 us, 600
+// TFLOP/s (a fifth of their tiles lie on the diagonal and take the loop that is not
+// a tile ahead, and a workgroup's first loads have nothing beside them).
 //
 // Grid: (kv heads) x (tile slots).  Sequence s has the slots from
 // floor(cu[s] g / BM) + s on: as many as its tiles, or one more, whatever the
@@ -557,7 +559,7 @@ __device__ __forceinline__ f32x2v* tile_ml(const AttnArgs& a, int at) {
 
 // Requests of more than 32 rows: the prompt kernel's loop over pages.  Bound as
 // that one is, and by the pieces' sums (written and read once more).  Chunks of
-// four prompts (about 450 tokens of 56 heads each over up to 8700 keys): 314 us.
+// four prompts (about 450 tokens of 56 heads each over up to 8700 keys): 320 us.
 template <typename T, int D, int DV, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
   typedef TileKernel<T, D, DV, NW, true> TK;
@@ -597,8 +599,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
 
 // Requests of at most 32 rows (single tokens above all): the waves take 32 keys
 // each of a tile of 32 NW, through two LDS stages of their own, and join their
-// sums at the end of a piece.  Bound by memory: nearly all of the LDS holds loads in
-// flight.  128 requests over 3.94 GB of cache 606 us (6.5 TB/s; a streaming read
+// sums at the end of a piece.  Bound by memory: a compute unit has 128 KB of loads in
+// flight with 128-wide heads, 120 with 192-wide ones, 64 with 64-wide ones (48
+// requests over 311 MB of those 67 us a call, 4.7 TB/s).  128 requests over 3.94 GB of cache 606 us (6.5 TB/s; a streaming read
 // reaches 6.95), 48 over 727 MB 115 us, one over 134 MB 26 us (ramp and the uneven
 // end of 8 or 9 tiles a workgroup).  Runs cut at 32 keys instead of 128 are more
 // even but slower (48 requests' calls 122 to 128 us, 100 over 1500 keys 67 to 74):
@@ -718,7 +721,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
       for (int i = 0; i < 16; i += 4)
         *(f32x4*)(so + 32 * b + 2 * i + 4 * h) =
             f32x4{rb.o[b][i] * f, rb.o[b][i + 1] * f, rb.o[b][i + 2] * f, rb.o[b][i + 3] * f};
-    // a row's joined statistics, in its last wave's slot once every wave has read it
+    // a row's joined statistics, in the first wave's slot once every wave has read it
     __syncthreads();
     if (wave == 0 && h == 0) {
       ml[0][lane][0] = M;
@@ -896,13 +899,14 @@ hipError_t launch_attn_prompt(AttnArgs a, int dtype, int D, hipStream_t s) {
     // Heads in turn leave an XCD's 64 places (two a compute unit) uneven at the
     // end: the last ones' longest tile starts when the others are nearly done.
     // So many at once that they give each place at least twice that tile's work (of
-    // slots (slots + 1) / 2 a head), and as many in the last group as in the others.
+    // slots (slots + 1) / 2 a head), in groups as equal as the count allows (five
+    // heads: three and two).
     // 128 heads of 192 over 2048 tokens: 16 heads an XCD 8 at once 198 us, one after
     // the other 206, all 16 (its L2 misses) 202; 64 heads over 4001 tokens 8 at once
     // 277, 4 at once 283; 32 over four prompts of 5000 tokens in all, 4 at once 125,
     // 3 and then 1 147.
     const long long heads = std::max(1, a.HK / 8), most = std::min<long long>(heads, (4 * 64 + slots) / (slots + 1));
-    const long long groups = (heads + std::max(1LL, most) - 1) / std::max(1LL, most);
+    const long long groups = (heads + most - 1) / most;
     a.heads_together = (int)((heads + groups - 1) / groups);
     kernel<<<(unsigned)(slots * a.HK), 64 * NW, TK::lds, s>>>(a);
     return hipGetLastError();

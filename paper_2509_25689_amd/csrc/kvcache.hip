@@ -10,7 +10,7 @@
 // writes is read by another: a token's page is looked up in the table below
 // `held` and in the ring from there on, and pages go back to ring places beyond
 // those taken.  Bound by the launch and a few dependent reads: one wave for 48
-// requests 3.3 us, 16 workgroups for 512 requests with 32768 new tokens 6.2 us.
+// requests 3.4 us, 16 workgroups for 512 requests with 32768 new tokens 6.2 us.
 #include "attention.h"
 #include "layout.h"
 
@@ -159,8 +159,8 @@ __global__ __launch_bounds__(NT) void plan_kernel(PlanArgs a, bool fill, bool po
 // One 16-byte chunk of one token a copy; a thread keeps its (head, chunk) and
 // takes U tokens, S apart, whose loads are all in flight together.  blockIdx.y:
 // keys, values.  Bound by memory: read and written once, 8192 tokens of 16 heads of
-// 128 (134 MB in all) 29.8 us, 4.5 TB/s; by the launch for a decode batch, 48 tokens
-// 2.6 us.
+// 128 (134 MB in all) 29.7 us, 4.5 TB/s, where a dense copy of as much takes 26.0; by
+// the launch for a decode batch, 48 tokens 2.6 us.
 template <int U>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, int S) {
   const bool val = blockIdx.y;
