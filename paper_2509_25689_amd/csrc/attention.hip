@@ -143,8 +143,8 @@ __device__ __forceinline__ const char* q_row(const AttnArgs& a, const Seq& s, co
 // there too, but l is NaN: where rows' parts are joined, l says whether there is one.)
 template <typename T>
 __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
-  constexpr float ln2 = 0.69314718055994531f;
-  return l == 0.0f ? -INFINITY : m * a.scale + (__logf(l) - T::kLift * ln2);
+  constexpr float unlift = 1.0f / (1 << (int)T::kLift);  // (exact, where a difference of logarithms rounds)
+  return l == 0.0f ? -INFINITY : m * a.scale + __logf(l * unlift);
 }
 
 template <typename T, int DV, int DB>

@@ -82,3 +82,22 @@ def test_paged(att, dtype, d, new, heads):
     out, lse = att.paged(_query(new * R, heads, dtype), kc, vc, cu, torch.tensor(lens, dtype=torch.int32).cuda(), table, max_new=new,
                          scale=LN2, return_lse=True)
     _check(out, lse, [m - new + j for m in lens for j in range(new)], d, dtype)
+
+
+@pytest.mark.parametrize("dtype", [HF, BF])
+@pytest.mark.parametrize("dims", [(64, 64), (128, 128), (192, 128)])
+def test_lse_of_equal_scores(att, dtype, dims):
+    """Scores of 0: the sum of a row's p + 1 weights is exact, a single one's logarithm is exactly 0 and the
+    others' within the logarithm's and one product's rounding, 2^-22 of it."""
+    n, (D, DV) = 700, dims
+    q, k, v = (torch.zeros((n, 1, d), dtype=dtype, device="cuda") for d in (D, D, DV))
+    want = torch.arange(1, n + 1, dtype=torch.float64).log()
+    _, lse = att.prompt(q, k, v, torch.tensor([0, n], dtype=torch.int32).cuda(), return_lse=True)
+    assert lse[0, 0].item() == 0.0
+    assert ((lse[:, 0].double().cpu() - want).abs() <= 2.0 ** -22 * want).all()
+    kc, vc = att.empty_cache(11, 64, 1, D, DV, dtype=dtype)
+    att.append(kc, vc, k, v, torch.arange(n, device="cuda").int())
+    lens = torch.tensor([1, 2, 3, 64, 500, n], dtype=torch.int32)
+    _, lse = att.paged(q[:6], kc, vc, torch.arange(7).int().cuda(), lens.cuda(), torch.arange(11).int().cuda().repeat(6, 1), max_new=1,
+                       return_lse=True)
+    assert ((lse[:, 0].double().cpu() - lens.double().log()).abs() <= 2.0 ** -22 * lens.double().log()).all()
