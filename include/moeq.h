@@ -573,6 +573,131 @@ moeq_status moeq_attn_paged(const moeq_attn* a, const moeq_rows* q, const moeq_k
 /* Bytes of its workspace, for any lengths (host only). */
 moeq_status moeq_attn_paged_workspace(const moeq_attn* a, int32_t max_new, uint64_t* bytes);
 
+/* ---- A cache of 8-bit codes ----
+ * k and v of a moeq_kv_cache may hold e4m3 codes (OCP 8-bit floating point: 4
+ * exponent bits, 3 of mantissa, no infinities) with a scale 2^e for every token's
+ * key and value of each head, held as the byte e + 127.  Strides are then in bytes,
+ * multiples of 16; the scale of (page, place, head) is at k[page * k_page_stride +
+ * head * k_head_stride + place], values' likewise.
+ *   k, v    DEVICE, on 16 bytes; strides in bytes, non-negative multiples of 16 */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t k_page_stride, k_head_stride;
+  int64_t v_page_stride, v_head_stride;
+} moeq_kv_scales;
+
+/* moeq_kv_append to such a cache.  A row's scale is the smallest 2^e (e >= -126)
+ * that takes its largest finite magnitude to 448 at most (1 for a row of zeros);
+ * its values times 2^-e are rounded to the nearest code, ties to even.  Infinities
+ * and NaN become NaN.  MOEQ_F16: a code that would stand for more than 65504 is the
+ * next smaller one.
+ *   a, k, v, slots, n_tokens  as for moeq_kv_append; the dims are multiples of 16
+ *                  up to 1024
+ *   cache, scales  (written) whose rows lie apart, as there
+ * Errors: INVALID_ARG, UNSUPPORTED, DEVICE. */
+moeq_status moeq_kv_append_e4m3(const moeq_attn* a, const moeq_kv_cache* cache, const moeq_kv_scales* scales,
+                                const moeq_rows* k, const moeq_rows* v, const int32_t* slots, int32_t n_tokens,
+                                void* stream);
+
+/* moeq_attn_paged over such a cache.  a's dtype is that of q and out; the products take
+ * codes and scales as the values they stand for, in dtype's range (a MOEQ_F16 cache is
+ * one that was written as such).  The scales' bytes lie in 1 .. 254.  Workspace and
+ * errors as for moeq_attn_paged. */
+moeq_status moeq_attn_paged_e4m3(const moeq_attn* a, const moeq_rows* q, const moeq_kv_cache* cache,
+                                 const moeq_kv_scales* scales, const int32_t* cu_q, const int32_t* kv_lens,
+                                 const int32_t* block_table, int64_t table_stride, int32_t max_blocks,
+                                 int32_t n_requests, int32_t n_tokens, int32_t max_new, const moeq_rows* out,
+                                 float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* ---- Drafted tokens ----
+ * A request's new tokens may be a tree of drafts: token 0 is the root, the token that
+ * the step would have had without drafts; parents[i] is the number (among the
+ * request's new tokens) of the token that token i was drafted to follow.  Anything but
+ * the number of an earlier token (-1 for the root) is no parent.  Their keys and values
+ * lie in the cache at the positions after the context in the order of the tokens, like
+ * those of a chunk; their positions in the text (context + depth) are the caller's to
+ * turn the queries and keys by.
+ *
+ * moeq_attn_tree is moeq_attn_paged where a new token sees the kv_lens[r] - n keys
+ * before the step's n = cu_q[r + 1] - cu_q[r], its own and its ancestors'.
+ *   scales   of a cache of codes, or NULL: of 16-bit values
+ *   parents  DEVICE int32 [n_tokens]
+ *   a        causal 1, window 0
+ *   max_new  at most 256 (else UNSUPPORTED)
+ * The rest, the workspace and the errors as for moeq_attn_paged. */
+moeq_status moeq_attn_tree(const moeq_attn* a, const moeq_rows* q, const moeq_kv_cache* cache,
+                           const moeq_kv_scales* scales, const int32_t* cu_q, const int32_t* kv_lens,
+                           const int32_t* parents, const int32_t* block_table, int64_t table_stride,
+                           int32_t max_blocks, int32_t n_requests, int32_t n_tokens, int32_t max_new,
+                           const moeq_rows* out, float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Which drafted tokens are kept, and the token that follows them, so that the tokens
+ * are distributed as if each had been drawn from the target alone.  target's row of
+ * token t is the distribution after t.  From the root on, the children of the token
+ * reached last are tried in their order against the residual r, at first target's row
+ * (taken to sum to z = 1):
+ *   with draft (row t: the distribution that t's children were drawn from), child c of
+ *   token x is kept if uniform[c] draft[t][x] z < r[x]; a rejected one leaves
+ *   max(r - z draft[t], 0), and z its sum;
+ *   with draft NULL (drafts that were not drawn: the likeliest tokens, a lookup's), it
+ *   is kept if uniform[c] z < r[x]; a rejected one leaves r with r[x] = 0, and z - r[x].
+ * Where no child is kept, the next token is the first j with r[0] + .. + r[j] > last[r] *
+ * sum r (where r is 0 throughout, of target's row; -1 where the sum is not finite and
+ * positive).  Products, residuals and sums are float64.
+ *   tokens    DEVICE int32 [n_tokens]: the drafted ones (the roots' are not read); one
+ *             outside 0 .. vocab - 1 is rejected
+ *   parents   DEVICE int32 [n_tokens], as above
+ *   cu        DEVICE int32 [n_requests + 1], ascending, within 0 .. n_tokens
+ *   max_new   0 .. 256: at least the most tokens of a request (a larger one is left out)
+ *   vocab     1 .. 2^20
+ *   target, draft  DEVICE float [n_tokens x vocab], rows target_stride (draft_stride) >=
+ *             vocab apart; draft may be NULL
+ *   uniform   DEVICE float [n_tokens], in [0, 1) (the roots' are not used)
+ *   last      DEVICE float [n_requests], in [0, 1)
+ *   path      DEVICE int32 [n_requests x max_new] (written): the numbers of the root and
+ *             the kept tokens, then -1
+ *   counts    DEVICE int32 [n_requests] (written): how many (0: no tokens, or left out)
+ *   out_tokens  DEVICE int32 [n_requests x max_new] (written): the kept tokens after the
+ *             root and the one that follows them (counts[r] tokens), then -1
+ *   workspace  DEVICE, on 256 bytes, at least moeq_verify_workspace's bytes; need not be
+ *             cleared, holds nothing between calls
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (workspace), DEVICE. */
+moeq_status moeq_verify(const int32_t* tokens, const int32_t* parents, const int32_t* cu, int32_t n_requests,
+                        int32_t n_tokens, int32_t max_new, int32_t vocab, const float* target, int64_t target_stride,
+                        const float* draft, int64_t draft_stride, const float* uniform, const float* last,
+                        int32_t* path, int32_t* counts, int32_t* out_tokens, void* workspace, uint64_t workspace_bytes,
+                        void* stream);
+/* Bytes of its workspace (host only). */
+moeq_status moeq_verify_workspace(int32_t n_requests, int32_t vocab, uint64_t* bytes);
+
+/* Keeps the tokens of a path in the cache: moves the key and value (and their scales)
+ * of position ctx_lens[r] + path[r][j] to ctx_lens[r] + j, j < counts[r].
+ *   cache, scales  as for moeq_kv_append (scales NULL) or moeq_kv_append_e4m3; (written)
+ *   path     DEVICE int32 [n_requests x max_path], rows path_stride apart: ascending from
+ *            0 on (moeq_verify's; of a row that is not, what is moved is unspecified, but
+ *            lies within the cache)
+ *   counts, ctx_lens  DEVICE int32 [n_requests]
+ *   block_table  as for moeq_attn_paged; positions in no page of the cache are left out
+ * No two requests' tables may share the pages behind their contexts.
+ * Errors: INVALID_ARG, UNSUPPORTED, DEVICE. */
+moeq_status moeq_kv_commit(const moeq_kv_cache* cache, const moeq_kv_scales* scales, int32_t n_kv_heads,
+                           int32_t head_dim, int32_t value_dim, const int32_t* path, int64_t path_stride,
+                           int32_t max_path, const int32_t* counts, const int32_t* ctx_lens,
+                           const int32_t* block_table, int64_t table_stride, int32_t max_blocks, int32_t n_requests,
+                           void* stream);
+
+/* Gives the pages that requests no longer need back to the ring of free pages: of
+ * request r's pages for kv_lens[r] tokens, those beyond the ones for its first
+ * kept_lens[r], to the ring's tail, in the requests' order.
+ *   kv_lens, kept_lens  DEVICE int32 [n_requests], at most 2^30
+ *   block_table, free_pages, pool_in, pool_out  as for moeq_kv_plan (the table is not
+ *            written); pool_out: head, pages free, 0
+ * Errors: INVALID_ARG, DEVICE. */
+moeq_status moeq_kv_trim(const int32_t* kv_lens, const int32_t* kept_lens, int32_t n_requests,
+                         const int32_t* block_table, int64_t table_stride, int32_t max_blocks, int32_t* free_pages,
+                         int32_t n_pages, const int32_t* pool_in, int32_t* pool_out, int32_t page_size, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -110,6 +110,30 @@ Cache cache(PyObject* ko, PyObject* vo, at::ScalarType dtype, const at::Tensor& 
                k.size(2), k.size(3), v.size(3)};
 }
 
+// A cache of codes has scales [pages, kv heads, page size], a pair of tensors; None: a
+// cache of `dtype`.
+struct Codes {
+  bool some;
+  moeq_kv_scales s;
+  const moeq_kv_scales* get() const { return some ? &s : nullptr; }
+};
+Codes scales(PyObject* o, const Cache& c, const at::Tensor& like) {
+  if (o == Py_None) return Codes{false, {}};
+  PyObject* two[2];
+  for (int i = 0; i < 2; ++i) two[i] = PyTuple_GET_ITEM(o, i);  // (cache_of has checked the pair)
+  const Shape s{{c.c.n_pages, c.heads, c.c.page_size}, 3};
+  const at::Tensor &k = check(two[0], "scales[0]", at::kFloat8_e8m0fnu, s, like),
+                   &v = check(two[1], "scales[1]", at::kFloat8_e8m0fnu, s, like);
+  return Codes{true, {k.data_ptr(), v.data_ptr(), stride_of(k, 0), stride_of(k, 1), stride_of(v, 0), stride_of(v, 1)}};
+}
+// The cache of a call with these scales (None: of dtype's values)
+Cache cache_of(PyObject* ko, PyObject* vo, PyObject* sc, at::ScalarType dtype, const at::Tensor& like) {
+  if (sc == Py_None) return cache(ko, vo, dtype, like);
+  if (!PyTuple_Check(sc) || PyTuple_GET_SIZE(sc) != 2)
+    throw Raise{PyExc_TypeError, "scales must be None or a tuple of two tensors"};
+  return cache(ko, vo, at::kFloat8_e4m3fn, like);
+}
+
 int32_t dtype_code(at::ScalarType t) {
   if (t == at::kBFloat16) return MOEQ_BF16;
   if (t == at::kHalf) return MOEQ_F16;
@@ -162,6 +186,12 @@ void done(moeq_status st) {
 // (Inference tensors have no count.)
 void written(const at::Tensor& t) {
   if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
+void cache_written(PyObject* k, PyObject* v, PyObject* sc) {
+  written(tensor(k, "k_cache"));
+  written(tensor(v, "v_cache"));
+  for (int i = 0; sc != Py_None && i < 2; ++i) written(tensor(PyTuple_GET_ITEM(sc, i), "scales"));
 }
 
 // out, if given, else a new tensor
@@ -221,17 +251,20 @@ PyObject* plan(PyObject* const* a) {
   return t;
 }
 
-// k_cache, v_cache, k, v, slots, stream
+// k_cache, v_cache, k, v, slots, scales, stream
 PyObject* append(PyObject* const* a) {
   const at::Tensor& k = first(a[2], "k");
   const at::ScalarType dt = k.scalar_type();
-  const Cache c = cache(a[0], a[1], dt, k);
+  const Cache c = cache_of(a[0], a[1], a[5], dt, k);
+  const Codes sc = scales(a[5], c, k);
   const int64_t T = k.dim() ? k.size(0) : 0;
   const moeq_rows kr = rows(a[2], "k", dt, T, c.heads, c.dim, k), vr = rows(a[3], "v", dt, T, c.heads, c.value_dim, k);
   const moeq_attn d = describe(c.heads, c.heads, c.dim, c.value_dim, dt);
-  done(moeq_kv_append(&d, &c.c, &kr, &vr, ints(a[4], "slots", T, k), narrow(T, "the number of tokens"), stream(a[5], k)));
-  written(tensor(a[0], "k_cache"));
-  written(tensor(a[1], "v_cache"));
+  const int32_t* slots = ints(a[4], "slots", T, k);
+  const int32_t n = narrow(T, "the number of tokens");
+  done(sc.some ? moeq_kv_append_e4m3(&d, &c.c, sc.get(), &kr, &vr, slots, n, stream(a[6], k))
+               : moeq_kv_append(&d, &c.c, &kr, &vr, slots, n, stream(a[6], k)));
+  cache_written(a[0], a[1], a[5]);
   Py_RETURN_NONE;
 }
 
@@ -262,13 +295,14 @@ PyObject* prompt(PyObject* const* a) {
   return with ? pair(out, lse) : THPVariable_Wrap(out);
 }
 
-// q, k_cache, v_cache, cu_q, kv_lens, block_table, max_new, causal, window, scale, out, lse, workspace, stream
+// q, k_cache, v_cache, cu_q, kv_lens, block_table, max_new, causal, window, scale, out, lse, workspace, scales, parents, stream
 PyObject* paged(PyObject* const* a) {
   const at::Tensor& q = first(a[0], "q");
   if (q.dim() != 3) refuse("q", "have three dimensions", q);
   const at::ScalarType dt = q.scalar_type();
   const int64_t T = q.size(0), heads = q.size(1), dim = q.size(2);
-  const Cache c = cache(a[1], a[2], dt, q);
+  const Cache c = cache_of(a[1], a[2], a[13], dt, q);
+  const Codes sc = scales(a[13], c, q);
   if (c.dim != dim) refuse("k_cache", "have keys as wide as q's rows, " + std::to_string(dim), tensor(a[1], "k_cache"));
   const at::Tensor& lens = tensor(a[4], "kv_lens");
   if (lens.dim() != 1) refuse("kv_lens", "have one dimension", lens);
@@ -291,11 +325,21 @@ PyObject* paged(PyObject* const* a) {
   at::Tensor lse;
   if (with) lse = output(a[11] == Py_True ? Py_None : a[11], "lse", at::kFloat, {T, heads}, q);
   const moeq_rows orow = rows(out);
-  const int64_t width = table.size(1);
-  done(moeq_attn_paged(&d, &qr, &c.c, cp, lp, (const int32_t*)table.data_ptr(), R > 1 ? table.stride(0) : width,
-                       narrow(width, "the table's width"), narrow(R, "the number of requests"),
-                       narrow(T, "the number of tokens"), max_new, &orow, with ? (float*)lse.data_ptr() : nullptr,
-                       ws.data_ptr(), (uint64_t)ws.numel(), stream(a[13], q)));
+  const int32_t width = narrow(table.size(1), "the table's width"), r = narrow(R, "the number of requests"),
+                t = narrow(T, "the number of tokens");
+  const int64_t pitch = R > 1 ? table.stride(0) : width;
+  const int32_t* tp = (const int32_t*)table.data_ptr();
+  float* lsep = with ? (float*)lse.data_ptr() : nullptr;
+  const uint64_t bytes = ws.numel();
+  void* on = stream(a[15], q);
+  if (a[14] != Py_None)
+    done(moeq_attn_tree(&d, &qr, &c.c, sc.get(), cp, lp, ints(a[14], "parents", T, q), tp, pitch, width, r, t, max_new,
+                        &orow, lsep, ws.data_ptr(), bytes, on));
+  else if (sc.some)
+    done(moeq_attn_paged_e4m3(&d, &qr, &c.c, sc.get(), cp, lp, tp, pitch, width, r, t, max_new, &orow, lsep,
+                              ws.data_ptr(), bytes, on));
+  else
+    done(moeq_attn_paged(&d, &qr, &c.c, cp, lp, tp, pitch, width, r, t, max_new, &orow, lsep, ws.data_ptr(), bytes, on));
   written(out);
   return with ? pair(out, lse) : THPVariable_Wrap(out);
 }
@@ -305,6 +349,98 @@ PyObject* paged_workspace(PyObject* const* a) {
   const moeq_attn d = describe(number(a[0]), number(a[1]), number(a[2]), number(a[3]), at::kBFloat16);
   uint64_t bytes = 0;
   done(moeq_attn_paged_workspace(&d, narrow(number(a[4]), "max_new"), &bytes));
+  return PyLong_FromUnsignedLongLong(bytes);
+}
+
+// k_cache, v_cache, path, counts, ctx_lens, block_table, scales, stream
+PyObject* commit(PyObject* const* a) {
+  const at::Tensor& k = first(a[0], "k_cache");
+  if (a[6] == Py_None) dtype_code(k.scalar_type());
+  const Cache c = cache_of(a[0], a[1], a[6], k.scalar_type(), k);
+  const Codes sc = scales(a[6], c, k);
+  const at::Tensor& path = check(a[2], "path", at::kInt, Shape{{kAny, kAny}, 2}, k);
+  const int64_t R = path.size(0), width = path.size(1);
+  const int32_t *cp = ints(a[3], "counts", R, k), *xp = ints(a[4], "ctx_lens", R, k);
+  const at::Tensor& table = check(a[5], "block_table", at::kInt, Shape{{R, kAny}, 2}, k);
+  const int64_t blocks = table.size(1);
+  done(moeq_kv_commit(&c.c, sc.get(), narrow(c.heads, "the number of kv heads"), narrow(c.dim, "the head dimension"),
+                      narrow(c.value_dim, "the value dimension"), (const int32_t*)path.data_ptr(),
+                      R > 1 ? path.stride(0) : width, narrow(width, "the paths' width"), cp, xp,
+                      (const int32_t*)table.data_ptr(), R > 1 ? table.stride(0) : blocks,
+                      narrow(blocks, "the table's width"), narrow(R, "the number of requests"), stream(a[7], k)));
+  cache_written(a[0], a[1], a[6]);
+  Py_RETURN_NONE;
+}
+
+// kv_lens, kept_lens, block_table, free_pages, pool, page_size, pool_out, stream
+PyObject* trim(PyObject* const* a) {
+  const at::Tensor& lens = first(a[0], "kv_lens");
+  if (lens.dim() != 1) refuse("kv_lens", "have one dimension", lens);
+  const int64_t R = lens.size(0);
+  const int32_t *lp = ints(a[0], "kv_lens", R, lens), *kp = ints(a[1], "kept_lens", R, lens);
+  const at::Tensor& table = check(a[2], "block_table", at::kInt, Shape{{R, kAny}, 2}, lens);
+  const at::Tensor& free = check(a[3], "free_pages", at::kInt, Shape{{kAny}, 1}, lens);
+  const int32_t* pool = ints(a[4], "pool", 3, lens);
+  const at::Tensor out = output(a[6], "pool_out", at::kInt, {3}, lens);
+  const int64_t width = table.size(1);
+  done(moeq_kv_trim(lp, kp, narrow(R, "the number of requests"), (const int32_t*)table.data_ptr(),
+                    R > 1 ? table.stride(0) : width, narrow(width, "the table's width"), (int32_t*)free.data_ptr(),
+                    narrow(free.size(0), "the number of pages"), pool, (int32_t*)out.data_ptr(),
+                    narrow(number(a[5]), "page_size"), stream(a[7], lens)));
+  written(free);
+  written(out);
+  return THPVariable_Wrap(out);
+}
+
+// tokens, parents, cu, target, draft, uniform, last, max_new, buffer, workspace, stream
+PyObject* verify(PyObject* const* a) {
+  const at::Tensor& target = first(a[3], "target");
+  const int64_t T = target.dim() == 2 ? target.size(0) : 0, V = target.dim() == 2 ? target.size(1) : 0;
+  check(a[3], "target", at::kFloat, Shape{{T, V}, 2}, target);
+  const at::Tensor& cu = tensor(a[2], "cu");
+  if (cu.dim() != 1 || cu.size(0) < 1) refuse("cu", "be a vector of at least one element", cu);
+  const int64_t R = cu.size(0) - 1;
+  const int32_t *cp = ints(a[2], "cu", R + 1, target), *tp = ints(a[0], "tokens", T, target),
+                *pp = ints(a[1], "parents", T, target);
+  const float* draft = nullptr;
+  int64_t draft_row = V;
+  if (a[4] != Py_None) {
+    const at::Tensor& d = check(a[4], "draft", at::kFloat, Shape{{T, V}, 2}, target);
+    draft = (const float*)d.data_ptr();
+    draft_row = T > 1 ? d.stride(0) : V;
+  }
+  const float *up = (const float*)check(a[5], "uniform", at::kFloat, Shape{{T}, 1}, target).data_ptr(),
+              *lp = (const float*)check(a[6], "last", at::kFloat, Shape{{R}, 1}, target).data_ptr();
+  const int64_t W = number(a[7]);
+  if (W < 0) throw Raise{PyExc_ValueError, "max_new must not be negative"};
+  const int32_t r = narrow(R, "the number of requests"), v = narrow(V, "the vocabulary"), w = narrow(W, "max_new");
+  uint64_t bytes = 0;
+  at::Tensor ws;
+  if (a[9] == Py_None) {
+    done(moeq_verify_workspace(r, v, &bytes));
+    ws = at::empty({(int64_t)bytes}, target.options().dtype(at::kByte));
+  } else {
+    ws = check(a[9], "workspace", at::kByte, Shape{{kAny}, 1}, target);
+  }
+  // one allocation for what is returned
+  const at::Tensor all = output(a[8], "buffer", at::kInt, {R * (2 * W + 1)}, target);
+  int32_t *path = (int32_t*)all.data_ptr(), *out = path + R * W, *counts = out + R * W;
+  done(moeq_verify(tp, pp, cp, r, narrow(T, "the number of tokens"), w, v, (const float*)target.data_ptr(),
+                   T > 1 ? target.stride(0) : V, draft, draft_row, up, lp, path, counts, out, ws.data_ptr(),
+                   (uint64_t)ws.numel(), stream(a[10], target)));
+  const std::vector<at::Tensor> parts = all.unsafe_split_with_sizes({R * W, R * W, R});
+  PyObject* t = PyTuple_New(3);
+  if (!t) throw PythonError{};
+  PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(parts[0].view({R, W})));
+  PyTuple_SET_ITEM(t, 1, THPVariable_Wrap(parts[2]));
+  PyTuple_SET_ITEM(t, 2, THPVariable_Wrap(parts[1].view({R, W})));
+  return t;
+}
+
+// n_requests, vocab
+PyObject* verify_workspace(PyObject* const* a) {
+  uint64_t bytes = 0;
+  done(moeq_verify_workspace(narrow(number(a[0]), "the number of requests"), narrow(number(a[1]), "the vocabulary"), &bytes));
   return PyLong_FromUnsignedLongLong(bytes);
 }
 
@@ -350,9 +486,10 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define MOEQ_METHOD(f, n) \
   { #f, (PyCFunction)(void (*)(void))call<f, n>, METH_FASTCALL, nullptr }
-PyMethodDef methods[] = {MOEQ_METHOD(plan, 10),  MOEQ_METHOD(append, 6),          MOEQ_METHOD(prompt, 10),
-                         MOEQ_METHOD(paged, 14), MOEQ_METHOD(paged_workspace, 5), MOEQ_METHOD(setup, 3),
-                         {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {MOEQ_METHOD(plan, 10),   MOEQ_METHOD(append, 7),           MOEQ_METHOD(prompt, 10),
+                         MOEQ_METHOD(paged, 16),  MOEQ_METHOD(paged_workspace, 5),  MOEQ_METHOD(commit, 8),
+                         MOEQ_METHOD(trim, 8),    MOEQ_METHOD(verify, 11),          MOEQ_METHOD(verify_workspace, 2),
+                         MOEQ_METHOD(setup, 3),   {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attention", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -39,6 +39,11 @@ struct Bf16 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
                                                    0, 0);
   }
+  // the two e4m3 codes in a dword's low (high) half times a power of two
+  template <bool HIGH>
+  static __device__ __forceinline__ uint32_t codes(uint32_t v, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, scale, HIGH));
+  }
   // two values rounded to nearest even, the first in the low half
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v){lo, hi}, bf16x2));
@@ -57,6 +62,10 @@ struct F16 {
   static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
                                                   0);
+  }
+  template <bool HIGH>
+  static __device__ __forceinline__ uint32_t codes(uint32_t v, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, scale, HIGH));
   }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v){lo, hi}, f16x2));
@@ -146,6 +155,7 @@ struct GranuleOffsets {
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)(MOEQ_LDS char*)p; }
 
 __device__ __forceinline__ u32x4 lds_read16(uint32_t a) { return *(const MOEQ_LDS u32x4*)(uintptr_t)a; }
+__device__ __forceinline__ void lds_write16(uint32_t a, u32x4 v) { *(MOEQ_LDS u32x4*)(uintptr_t)a = v; }
 // Lane l of a group of 16 gets column l of the 4 rows x 16 columns whose row y
 // the group's lanes 4 y .. 4 y + 3 point at.
 __device__ __forceinline__ u32x2 lds_read_tr(uint32_t a) {
@@ -165,6 +175,27 @@ __device__ __forceinline__ float sum_halves(float v) {
 }
 
 constexpr float kLowest = -3.40282347e38f;
+
+// A row of 16-bit values in memory: 8 of them from 8 c on, 4 from 4 c on
+struct Row16 {
+  const char* p;
+  __device__ __forceinline__ u32x4 chunk(int c) const { return *gptr((const u32x4*)(p + 16 * c)); }
+  __device__ __forceinline__ u32x2 four(int c) const { return *gptr((const u32x2*)(p + 8 * c)); }
+};
+// of e4m3 codes
+template <typename T>
+struct Row8 {
+  const char* p;
+  float scale;
+  __device__ __forceinline__ u32x2 four(int c) const {
+    const uint32_t v = *gptr((const uint32_t*)(p + 4 * c));
+    return u32x2{T::template codes<false>(v, scale), T::template codes<true>(v, scale)};
+  }
+  __device__ __forceinline__ u32x4 chunk(int c) const {
+    const u32x2 x = four(2 * c), y = four(2 * c + 1);
+    return u32x4{x.x, x.y, y.x, y.y};
+  }
+};
 
 // One wave's state for 32 query rows; the lane's row is lane % 32.
 template <typename T, int D, int DV>
@@ -247,6 +278,13 @@ struct RowBlock {
       s[i] = (uint32_t)(at + 8 * (i / 4) + i % 4) < span ? s[i] : -INFINITY;
   }
 
+  // keys of a block whose bit is clear do not count
+  static __device__ __forceinline__ void mask_bits(f32x16& s, uint32_t bits) {
+    const uint32_t mine = bits >> ((threadIdx.x >> 5 & 1) * 4);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = mine >> (8 * (i / 4) + i % 4) & 1 ? s[i] : -INFINITY;
+  }
+
   // c = scale * log2(e).  The rows' running maximum moves only where a score
   // passes it by more than 2^kSlack in the exponential: the quotient O / l is
   // the same for any m, sums and P stay in range, and the 16 DB multiplications
@@ -305,8 +343,9 @@ struct RowBlock {
   // among its values is NaN.  So the key tiles that need a mask come first, and
   // where o is not finite after them it is formed anew, key by key on the vector
   // units, from the keys each row sees among the `width` keys of each of `tiles`
-  // tiles, tile_key(i) the first; key_row(key) and value_row(key) point at a
-  // key's rows (global), keys from `end` on do not exist.  m and l hold already.
+  // tiles, tile_key(i) the first; a row sees a key of [lo, hi) if sees(key).  Keys from
+  // `end` on do not exist.  keys.chunk(key, c) are 8 values of a key, keys.four(key, c)
+  // 4 of its value (from memory).  m and l hold already.
   __device__ __forceinline__ bool finite() const {
     // (largest magnitude; a NaN makes the sum NaN)
     float t = 0.0f;
@@ -316,9 +355,9 @@ struct RowBlock {
       for (int i = 0; i < 16; ++i) t = fmaf(o[b][i], 0.0f, t);
     return !__any(t != t);
   }
-  template <typename FT, typename FK, typename FV>
-  __device__ __forceinline__ void redo(float c, int lo, int hi, int tiles, int width, int end, FT tile_key, FK key_row,
-                                       FV value_row) {
+  template <typename K, typename FT, typename FS>
+  __device__ __forceinline__ void redo(float c, int lo, int hi, int tiles, int width, int end, const K& keys, FT tile_key,
+                                       FS sees) {
     const int h = (threadIdx.x >> 5) & 1;
 #pragma unroll
     for (int b = 0; b < DB; ++b) {
@@ -329,13 +368,13 @@ struct RowBlock {
       for (int tile = 0; tile < tiles; ++tile)
 #pragma unroll 1
         for (int key = tile_key(tile), stop = min(key + width, end); key < stop; ++key) {
-          const char* kr = key_row(key) + 16 * h;
+          const auto kr = keys.key_row(key);
           float s = 0.0f;
 #pragma unroll
           for (int t = 0; t < KS; ++t) {
             u32x4 y = q[t];
             asm volatile("" : "+v"(y));  // (or the unpacked queries stay in registers throughout)
-            const u32x4 x = *gptr((const u32x4*)(kr + 32 * t));
+            const u32x4 x = kr.chunk(2 * t + h);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               s = fmaf(T::low(x[j]), T::low(y[j]), s);
@@ -344,11 +383,11 @@ struct RowBlock {
           }
           s = sum_halves(s);
           const float w = T::low(T::pack(exp2_fast(fmaf(s, c, neg_mc)), 0.0f));
-          const bool seen = key >= lo && key < hi;
-          const char* vr = value_row(key) + 64 * b + 8 * h;
+          const bool seen = key >= lo && key < hi && sees(key);
+          const auto vr = keys.value_row(key);
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const u32x2 v = *gptr((const u32x2*)(vr + 16 * g));
+            const u32x2 v = vr.four(8 * b + h + 2 * g);
             e[4 * g + 0] += seen ? w * T::low(v.x) : 0.0f;
             e[4 * g + 1] += seen ? w * T::high(v.x) : 0.0f;
             e[4 * g + 2] += seen ? w * T::low(v.y) : 0.0f;

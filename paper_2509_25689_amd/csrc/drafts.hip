@@ -1,0 +1,324 @@
+// Which drafted tokens are kept, and the token that follows them.
+//
+// A request's tokens form a tree (the root is the last token before them); target[t]
+// is the distribution after token t, draft[t] the one that t's children were drawn
+// from.  From the root on, the children of the token that was reached last are tried
+// in their order against the residual r (at first target's row, of sum z = 1): child c
+// of token x is kept if uniform[c] draft(x) z < r(x), and rejected leaves
+//   r' = max(r - z draft, 0), z' = sum r'.
+// Without draft rows (drafts that were not drawn) it is kept if uniform[c] z < r(x),
+// and rejected leaves r with r(x) = 0, z' = z - r(x).  Where no child is kept the next
+// token is the first j with r_0 + .. + r_j > last z.  All of it is in float64: the
+// products uniform * draft are exact, and the sums' order moves no border that 2^-24
+// wide random numbers are likely to meet.
+#include "attention.h"
+#include "layout.h"
+
+namespace moeq {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = 16;                    // neighbours of a row that a thread takes
+constexpr int kPart = kThreads * kPer;     // of a row, one workgroup's
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
+  return v;
+}
+// the workgroup's sum, for every thread; tmp: a double for each wave
+__device__ __forceinline__ double group_sum(double v, double* tmp) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  v = wave_sum(v);
+  __syncthreads();
+  if (lane == 0) tmp[wave] = v;
+  __syncthreads();
+  double all = 0.0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) all += tmp[w];
+  return all;
+}
+
+// Values j .. j + kPer - 1 of a row, 0 beyond its end
+__device__ __forceinline__ void read_row(const float* row, int j, int V, float (&x)[kPer]) {
+  if (j + kPer <= V) {
+#pragma unroll
+    for (int i = 0; i < kPer; i += 4) {
+      const f32x4u v = *(const MOEQ_GLOBAL f32x4u*)(row + j + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i + e] = v[e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = j + i < V ? row[j + i] : 0.0f;
+  }
+}
+
+// the residual after n rejections, from the sums before each
+__device__ __forceinline__ double residual(float p, float q, const double* z, int n) {
+  double r = p;
+  for (int k = 0; k < n; ++k) {
+    const double d = r - z[k] * (double)q;
+    r = d > 0.0 || d != d ? d : 0.0;
+  }
+  return r;
+}
+
+// One workgroup a request: the walk.  Every wave takes the same way; where a sibling
+// after a rejected one is tried, the whole workgroup sums the residual.
+__global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
+  __shared__ int parent[kMaxTree], token[kMaxTree];
+  __shared__ float px[kMaxTree], qx[kMaxTree], u[kMaxTree];
+  __shared__ double z[kMaxTree], tmp[kThreads / 64];
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int first = min(max(a.cu[r], 0), a.T), n = min(max(a.cu[r + 1], first), a.T) - first;
+  int32_t *path = a.path + (int64_t)r * a.width, *out = a.out + (int64_t)r * a.width;
+  VerifyEnd* end = a.end + r;
+  if (n < 1 || n > kMaxTree || n > a.width) {  // nothing to keep, or left out
+    for (int i = tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
+    if (tid == 0) {
+      a.counts[r] = 0;
+      end->node = -1;
+    }
+    return;
+  }
+  static_assert(kThreads >= kMaxTree, "a thread a token");
+  if (tid < n) {
+    const int p = a.parents[first + tid], x = a.tokens[first + tid];
+    const bool child = p >= 0 && p < tid, there = child && (uint32_t)x < (uint32_t)a.V;
+    parent[tid] = child ? p : -1;
+    token[tid] = x;
+    px[tid] = there ? a.target[(int64_t)(first + p) * a.target_row + x] : 0.0f;
+    qx[tid] = there && a.draft ? a.draft[(int64_t)(first + p) * a.draft_row + x] : 1.0f;
+    u[tid] = a.uniform[first + tid];
+  }
+  __syncthreads();
+  int at = 0, count = 1, rejected = 0;
+  if (tid == 0) path[0] = 0;
+  for (int next = 1; next >= 0;) {  // the children of `at`
+    next = -1;
+    rejected = 0;
+    double total = 1.0;
+    for (int c0 = (at + 1) & ~63; c0 < n && next < 0; c0 += 64) {
+      uint64_t some = __ballot(c0 + lane < n && parent[min(c0 + lane, n - 1)] == at);
+      while (some) {
+        const int c = c0 + __builtin_ctzll(some);
+        some &= some - 1;
+        const int x = token[c];
+        const bool there = (uint32_t)x < (uint32_t)a.V;
+        double rx = px[c];
+        if (a.draft) {
+          if (rejected > 0) {
+            // (siblings after a rejected one alone take a pass over the row)
+            const float *p = a.target + (int64_t)(first + at) * a.target_row, *q = a.draft + (int64_t)(first + at) * a.draft_row;
+            double sum = 0.0;
+            for (int j = tid * kPer; j < a.V; j += kPart) {
+              float pv[kPer], qv[kPer];
+              read_row(p, j, a.V, pv);
+              read_row(q, j, a.V, qv);
+#pragma unroll
+              for (int i = 0; i < kPer; ++i) sum += residual(pv[i], qv[i], z, rejected);
+            }
+            total = group_sum(sum, tmp);
+            rx = residual(px[c], qx[c], z, rejected);
+          }
+        } else if (there && rejected > 0) {
+          // what an earlier sibling of the same token took
+          for (int b = at + 1; b < c; ++b)
+            if (parent[b] == at && token[b] == x) rx = 0.0;
+        }
+        if (there && (double)u[c] * (double)qx[c] * total < rx) {
+          next = c;
+          break;
+        }
+        if (a.draft) {
+          __syncthreads();
+          if (tid == 0) z[rejected] = total;
+          __syncthreads();
+        } else {
+          total -= rx;
+        }
+        ++rejected;
+      }
+    }
+    if (next >= 0) {
+      at = next;
+      if (tid == 0) {
+        path[count] = at;
+        out[count - 1] = token[at];
+      }
+      ++count;
+    }
+  }
+  for (int i = count + tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
+  if (tid == 0) {
+    a.counts[r] = count;
+    end->node = at;
+    end->rejected = rejected;
+    end->first = first;
+    end->n = n;
+  }
+  if (a.draft && tid < rejected) end->z[tid] = z[tid];
+}
+
+// The last residual: of chunk `chunk` of the row that a request ended
+// at, this thread's kPer values.  gone, z: LDS.
+struct Last {
+  double r[kPer];
+  __device__ __forceinline__ double sum() const {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) s += r[i];
+    return s;
+  }
+  __device__ __forceinline__ void read(const VerifyArgs& a, const VerifyEnd* end, int chunk, bool whole, int* gone,
+                                       int* n_gone, double* z) {
+    const int tid = threadIdx.x, j = chunk * kPart + tid * kPer;
+    const int node = end->node, first = end->first, rejected = whole ? 0 : end->rejected;
+    float p[kPer], q[kPer];
+    read_row(a.target + (int64_t)(first + node) * a.target_row, j, a.V, p);
+    if (a.draft && rejected) {
+      read_row(a.draft + (int64_t)(first + node) * a.draft_row, j, a.V, q);
+      if (tid < rejected) z[tid] = end->z[tid];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) r[i] = residual(p[i], q[i], z, rejected);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) r[i] = p[i];
+      if (rejected) {
+        // the node's children's tokens that lie in this chunk
+        if (tid == 0) *n_gone = 0;
+        __syncthreads();
+        if (tid < end->n && a.parents[first + tid] == node && tid > node) {
+          const int x = a.tokens[first + tid];
+          if ((uint32_t)x < (uint32_t)a.V && x / kPart == chunk) gone[atomicAdd(n_gone, 1)] = x;
+        }
+        __syncthreads();
+        for (int g = 0; g < *n_gone; ++g)
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) r[i] = gone[g] == j + i ? 0.0 : r[i];
+      }
+    }
+  }
+};
+
+// The residual's sum over one chunk of the row: workgroup (chunk, request)
+__global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
+  __shared__ int gone[kMaxTree], n_gone;
+  __shared__ double z[kMaxTree], tmp[kThreads / 64];
+  const int chunk = blockIdx.x % a.n_chunks, r = blockIdx.x / a.n_chunks;
+  const VerifyEnd* end = a.end + r;
+  if (end->node < 0) return;
+  Last last;
+  last.read(a, end, chunk, false, gone, &n_gone, z);
+  const double s = group_sum(last.sum(), tmp);
+  if (threadIdx.x == 0) a.sums[(int64_t)r * a.n_chunks + chunk] = s;
+}
+
+// The sums of the threads' values before this one's, and of all
+struct Scan {
+  double before, all;
+};
+__device__ __forceinline__ Scan group_scan(double own, double* tmp) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double incl = own;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const double o = __shfl_up(incl, d, 64);
+    if (lane >= d) incl += o;
+  }
+  __syncthreads();
+  if (lane == 63) tmp[wave] = incl;
+  __syncthreads();
+  Scan s{0.0, 0.0};
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < wave) s.before += tmp[w];
+    s.all += tmp[w];
+  }
+  s.before += incl - own;
+  return s;
+}
+
+// The token that follows: one workgroup a request finds the chunk by the sums, then
+// the place in it.
+__global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
+  __shared__ int gone[kMaxTree], n_gone, found, some;
+  __shared__ double z[kMaxTree], tmp[kThreads / 64], ahead, sums[kThreads];
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const VerifyEnd* end = a.end + r;
+  if (end->node < 0) return;
+  const double last = a.last[r];
+  Last row;
+  int token = -1;
+  for (int whole = 0; whole < 2; ++whole) {  // the residual; where nothing is left of it, the target's row
+    double own = 0.0;  // of chunk tid
+    if (!whole) {
+      if (tid < a.n_chunks) own = a.sums[(int64_t)r * a.n_chunks + tid];
+    } else {
+      for (int c = 0; c < a.n_chunks; ++c) {
+        row.read(a, end, c, true, gone, &n_gone, z);
+        const double s = group_sum(row.sum(), tmp);
+        if (tid == 0) sums[c] = s;
+      }
+      __syncthreads();
+      if (tid < a.n_chunks) own = sums[tid];
+    }
+    if (tid == 0) found = some = -1;
+    const Scan in = group_scan(own, tmp);  // (of chunk tid)
+    if (in.all == 0.0) continue;
+    if (!(in.all > 0.0 && in.all < INFINITY)) break;
+    const double goal = last * in.all;
+    // the first chunk that passes the goal; the last that holds anything, if rounding leaves none
+    if (own > 0.0) {
+      atomicMax(&some, tid);
+      if (in.before + own > goal) atomicMin((unsigned*)&found, (unsigned)tid);
+    }
+    __syncthreads();
+    const bool passed = found >= 0;
+    const int c = passed ? found : some;
+    if (tid == c) ahead = in.before;
+    __syncthreads();
+    if (tid == 0) found = some = -1;
+    if (c < 0) break;  // (sums below 0 among them)
+    row.read(a, end, c, whole, gone, &n_gone, z);
+    const Scan at = group_scan(row.sum(), tmp);
+    double t = ahead + at.before;
+    int mine = -1, positive = -1;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      t += row.r[i];
+      if (row.r[i] > 0.0) {
+        positive = c * kPart + tid * kPer + i;
+        if (t > goal && mine < 0) mine = positive;
+      }
+    }
+    if (passed && mine >= 0) atomicMin((unsigned*)&found, (unsigned)mine);
+    if (positive >= 0) atomicMax(&some, positive);
+    __syncthreads();
+    token = found >= 0 ? found : some;
+    break;
+  }
+  if (tid == 0) a.out[(int64_t)r * a.width + a.counts[r] - 1] = token;
+}
+
+}  // namespace
+
+// (at most one for each thread of verify_pick_kernel)
+int verify_chunks(int V) { return (V + kPart - 1) / kPart; }
+
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
+  verify_walk_kernel<<<a.R, kThreads, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  verify_sums_kernel<<<(unsigned)((int64_t)a.R * a.n_chunks), kThreads, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  verify_pick_kernel<<<a.R, kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace moeq

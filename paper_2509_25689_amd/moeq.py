@@ -92,6 +92,12 @@ class moeq_kv_cache(ctypes.Structure):
                 ("v_slot_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64)]
 
 
+class moeq_kv_scales(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_page_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+                ("v_page_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build()")
@@ -104,7 +110,8 @@ def _load():
         pass
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, I64, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-    ATTN, ROWS, CACHE = (ctypes.POINTER(c) for c in (moeq_attn, moeq_rows, moeq_kv_cache))
+    ATTN, ROWS, CACHE, SCALES = (ctypes.POINTER(c) for c in (moeq_attn, moeq_rows, moeq_kv_cache, moeq_kv_scales))
+    U64 = ctypes.c_uint64
     sig = {
         "moeq_layer_create": [ctypes.POINTER(moeq_config), P, P, P, P, I32, ctypes.POINTER(P)],
         "moeq_forward": [P, P, P, I32, P, P],
@@ -133,6 +140,13 @@ def _load():
         "moeq_attn_prompt": [ATTN, ROWS, ROWS, ROWS, P, I32, I32, ROWS, P, P],
         "moeq_attn_paged": [ATTN, ROWS, CACHE, P, P, P, I64, I32, I32, I32, I32, ROWS, P, P, ctypes.c_uint64, P],
         "moeq_attn_paged_workspace": [ATTN, I32, ctypes.POINTER(ctypes.c_uint64)],
+        "moeq_kv_append_e4m3": [ATTN, CACHE, SCALES, ROWS, ROWS, P, I32, P],
+        "moeq_attn_paged_e4m3": [ATTN, ROWS, CACHE, SCALES, P, P, P, I64, I32, I32, I32, I32, ROWS, P, P, U64, P],
+        "moeq_attn_tree": [ATTN, ROWS, CACHE, SCALES, P, P, P, P, I64, I32, I32, I32, I32, ROWS, P, P, U64, P],
+        "moeq_verify": [P, P, P, I32, I32, I32, I32, P, I64, P, I64, P, P, P, P, P, P, U64, P],
+        "moeq_verify_workspace": [I32, I32, ctypes.POINTER(U64)],
+        "moeq_kv_commit": [CACHE, SCALES, I32, I32, I32, P, I64, I32, P, P, P, I64, I32, I32, P],
+        "moeq_kv_trim": [P, P, I32, P, I64, I32, P, I32, P, P, I32, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -313,6 +327,53 @@ def moeq_attn_paged_workspace(attn, max_new):
     b = ctypes.c_uint64()
     _check(lib.moeq_attn_paged_workspace(attn, max_new, ctypes.byref(b)))
     return b.value
+
+
+def moeq_kv_append_e4m3(attn, cache, scales, k, v, slots, n_tokens, stream=0):
+    """As moeq_kv_append; scales: moeq_kv_scales."""
+    _check(lib.moeq_kv_append_e4m3(attn, cache, scales, k, v, slots, n_tokens, stream or None))
+
+
+def moeq_attn_paged_e4m3(attn, q, cache, scales, cu_q, kv_lens, block_table, table_stride, max_blocks, n_requests, n_tokens,
+                         max_new, out, lse, workspace, workspace_bytes, stream=0):
+    """As moeq_attn_paged; scales: moeq_kv_scales."""
+    _check(lib.moeq_attn_paged_e4m3(attn, q, cache, scales, cu_q, kv_lens, block_table, table_stride, max_blocks,
+                                    n_requests, n_tokens, max_new, out, lse or None, workspace, workspace_bytes, stream or None))
+
+
+def moeq_attn_tree(attn, q, cache, scales, cu_q, kv_lens, parents, block_table, table_stride, max_blocks, n_requests,
+                   n_tokens, max_new, out, lse, workspace, workspace_bytes, stream=0):
+    """As moeq_attn_paged; scales: moeq_kv_scales or None; parents: device address."""
+    _check(lib.moeq_attn_tree(attn, q, cache, scales, cu_q, kv_lens, parents, block_table, table_stride, max_blocks,
+                              n_requests, n_tokens, max_new, out, lse or None, workspace, workspace_bytes, stream or None))
+
+
+def moeq_verify(tokens, parents, cu, n_requests, n_tokens, max_new, vocab, target, target_stride, draft, draft_stride,
+                uniform, last, path, counts, out_tokens, workspace, workspace_bytes, stream=0):
+    """Every array a device address (draft may be 0)."""
+    _check(lib.moeq_verify(tokens, parents, cu, n_requests, n_tokens, max_new, vocab, target, target_stride, draft or None,
+                           draft_stride, uniform, last, path, counts, out_tokens, workspace, workspace_bytes, stream or None))
+
+
+def moeq_verify_workspace(n_requests, vocab):
+    """Bytes of moeq_verify's workspace."""
+    b = ctypes.c_uint64()
+    _check(lib.moeq_verify_workspace(n_requests, vocab, ctypes.byref(b)))
+    return b.value
+
+
+def moeq_kv_commit(cache, scales, n_kv_heads, head_dim, value_dim, path, path_stride, max_path, counts, ctx_lens, block_table,
+                   table_stride, max_blocks, n_requests, stream=0):
+    """cache: moeq_kv_cache; scales: moeq_kv_scales or None; the arrays device addresses."""
+    _check(lib.moeq_kv_commit(cache, scales, n_kv_heads, head_dim, value_dim, path, path_stride, max_path, counts, ctx_lens,
+                              block_table, table_stride, max_blocks, n_requests, stream or None))
+
+
+def moeq_kv_trim(kv_lens, kept_lens, n_requests, block_table, table_stride, max_blocks, free_pages, n_pages, pool_in, pool_out,
+                 page_size, stream=0):
+    """Every array a device address."""
+    _check(lib.moeq_kv_trim(kv_lens, kept_lens, n_requests, block_table, table_stride, max_blocks, free_pages, n_pages,
+                            pool_in, pool_out, page_size, stream or None))
 
 
 def expert_importance(shape, logits, *, alpha, retain, bias=None, stream=None):
