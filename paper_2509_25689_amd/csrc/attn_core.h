@@ -162,6 +162,13 @@ __device__ __forceinline__ u32x2 lds_read_tr(uint32_t a) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((MOEQ_LDS s16x4*)(uintptr_t)a));
 }
 
+// The same of bytes: column l of the 8 rows x 16 columns whose row y the group's lanes
+// 2 y and 2 y + 1 point at, 8 bytes each.
+typedef int i32x2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32x2 lds_read_tr8(uint32_t a) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((MOEQ_LDS i32x2v*)(uintptr_t)a));
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // f(v of this lane, v of the lane 32 away)
@@ -197,8 +204,10 @@ struct Row8 {
   }
 };
 
-// One wave's state for 32 query rows; the lane's row is lane % 32.
-template <typename T, int D, int DV>
+// One wave's state for 32 query rows; the lane's row is lane % 32.  CODES: the keys
+// are read as 16 codes at a time, so a step's halves of the wave take 8 dims each of
+// two neighbouring 16.
+template <typename T, int D, int DV, bool CODES = false>
 struct RowBlock {
   static constexpr int KS = D / 16;    // steps of the first product
   static constexpr int DB = DV / 32;   // blocks of 32 value columns
@@ -223,8 +232,10 @@ struct RowBlock {
   __device__ __forceinline__ void load_q(const char* row) {
     const int h = (threadIdx.x >> 5) & 1;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) q[s] = row ? *gptr((const u32x4*)(row + (2 * s + h) * 16)) : u32x4{0, 0, 0, 0};
+    for (int s = 0; s < KS; ++s) q[s] = row ? *gptr((const u32x4*)(row + q_chunk(s, h) * 16)) : u32x4{0, 0, 0, 0};
   }
+  // the 8 dims that half h of the wave holds for step s
+  static __device__ __forceinline__ int q_chunk(int s, int h) { return CODES ? 4 * (s >> 1) + 2 * h + (s & 1) : 2 * s + h; }
 
   // the lane's LDS offsets inside a tile whose first row is a multiple of 16
   struct Addr {
@@ -374,7 +385,7 @@ struct RowBlock {
           for (int t = 0; t < KS; ++t) {
             u32x4 y = q[t];
             asm volatile("" : "+v"(y));  // (or the unpacked queries stay in registers throughout)
-            const u32x4 x = kr.chunk(2 * t + h);
+            const u32x4 x = kr.chunk(q_chunk(t, h));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               s = fmaf(T::low(x[j]), T::low(y[j]), s);

@@ -679,6 +679,79 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
   });
 }
 
+// floats of a row where a workgroup's waves join their sums
+template <int DV>
+constexpr int kFewPitch = DV + 4;
+
+// Joins the waves' sums of a piece's rows (o, m and each lane's half of l) and writes
+// the rows, or the piece's part of them.  smem: wave_bytes for each wave, kFewRows rows
+// at least, read and written by its wave alone so far; the caller waits before the
+// next piece.
+template <typename T, int DV, int NW>
+__device__ __forceinline__ void few_finish(const AttnArgs& a, const f32x16 (&o)[DV / 32], float m_own, float l_half,
+                                           char* smem, uint32_t wave_bytes, float (&ml)[NW][kFewRows][2], const Seq& s,
+                                           int kvh, bool whole, int slot) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  const float l = sum_halves(l_half);
+  if (h == 0) {
+    ml[wave][lane][0] = m_own;
+    ml[wave][lane][1] = l;
+  }
+  __syncthreads();
+  float M = kLowest, L = 0.0f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w][lane & 31][0]);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const float mw = ml[w][lane & 31][0], lw = ml[w][lane & 31][1];
+    L += lw == 0.0f ? 0.0f : lw * exp2_fast((mw - M) * a.c);
+  }
+  const float f = m_own == kLowest ? 0.0f : exp2_fast((m_own - M) * a.c);
+  float* so = (float*)(smem + wave * wave_bytes) + (lane & 31) * kFewPitch<DV>;
+#pragma unroll
+  for (int b = 0; b < DV / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *(f32x4*)(so + 32 * b + 2 * i + 4 * h) =
+          f32x4{o[b][i] * f, o[b][i + 1] * f, o[b][i + 2] * f, o[b][i + 3] * f};
+  // a row's joined statistics, in the first wave's slot once every wave has read it
+  __syncthreads();
+  if (wave == 0 && h == 0) {
+    ml[0][lane][0] = M;
+    ml[0][lane][1] = L;
+  }
+  __syncthreads();
+  const int rows = s.n * a.g;
+  for (int i = tid; i < rows * (DV / 8); i += 64 * NW) {
+    const int rr = i / (DV / 8), col = i % (DV / 8) * 8;
+    f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float* p = (const float*)(smem + w * wave_bytes) + rr * kFewPitch<DV> + col;
+      x += *(const f32x4*)p;
+      y += *(const f32x4*)(p + 4);
+    }
+    const float m = ml[0][rr][0], lr = ml[0][rr][1];
+    if (whole) {
+      const float inv = lr > 0.0f || !(lr == lr) ? 1.0f / lr : 0.0f;
+      const int token = div_g(a, rr), head = kvh * a.g + rr - token * a.g;
+      *(u32x4*)(a.out + (int64_t)(s.start + token) * a.o_row + (int64_t)head * a.o_head + col * 2) =
+          u32x4{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv), T::pack(y[0] * inv, y[1] * inv),
+                T::pack(y[2] * inv, y[3] * inv)};
+      if (a.lse && col == 0)
+        a.lse[(int64_t)(s.start + token) * a.HQ + head] = log_sum<T>(a, m, lr);
+    } else {
+      const int64_t at = (int64_t)slot * kFewRows + rr;
+      *(f32x4*)(a.few_part + at * DV + col) = x;
+      *(f32x4*)(a.few_part + at * DV + col + 4) = y;
+      if (col == 0) {
+        a.few_ml[2 * at] = m;
+        a.few_ml[2 * at + 1] = lr;
+      }
+    }
+  }
+}
+
 // Requests of at most 32 rows (single tokens above all): the waves take 32 keys
 // each of a tile of 32 NW, through two LDS stages of their own, and join their
 // sums at the end of a piece.  Bound by memory: a compute unit has 128 KB of loads in
@@ -693,12 +766,11 @@ struct FewKernel {
   static constexpr int BN = 32 * NW;
   static constexpr uint32_t kK = 32 * D * 2, kV = 32 * DV * 2, kStage = kK + kV, kWave = 2 * kStage;
   static constexpr int kLoads = 2 * (D / 32 + DV / 32);  // of a stage
-  static constexpr int kPitch = DV + 4;                  // floats of a row in the join
   static constexpr size_t lds = NW * kWave;
-  static_assert(kFewRows * kPitch * 4 <= kWave, "a wave's sums fit its stages");
+  static_assert(kFewRows * kFewPitch<DV> * 4 <= kWave, "a wave's sums fit its stages");
 };
 
-template <typename T, int D, int DV, int NW, bool E4M3, bool TREE>
+template <typename T, int D, int DV, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
   typedef FewKernel<T, D, DV, NW> FK;
   typedef RowBlock<T, D, DV> RB;
@@ -707,13 +779,12 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
   extern __shared__ __align__(128) char smem[];  // (16-byte accesses, after any static LDS)
   __shared__ float ml[NW][kFewRows][2];
   __shared__ int tmp[NW + 5], parents[TREE ? kMaxTree : 1];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t mine = lds_addr(smem) + wave * FK::kWave;
   RB rb;
   typename RB::Addr ad;
   ad.set();
-  std::conditional_t<E4M3, Keys8<T, D, DV>, Keys<D, DV, true, true>> keys(a);
+  Keys<D, DV, true, true> keys(a);
   each_piece<W, 64 * NW>(a, tmp, a.few_join, [&](int kvh, int r, const Seq& s, int, const Span& sp, int t0, int n, bool whole, int slot) {
     keys.seq(s, r, kvh);
     const Order od(sp.lo + t0 * FK::BN + wave * 32, min(sp.hi, sp.lo + (t0 + n) * FK::BN), FK::BN, 32,
@@ -785,65 +856,241 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
     if (od.masked > 0 && !rb.finite())
       rb.redo(a.c, row.see.lo, top, od.masked, 32, s.kv, keys, [&](int i) { return od.key(i); }, see);
     for (int i = od.masked; i < od.n; ++i) tile(i, false);
-    // join the waves
-    const float l = sum_halves(rb.l);
-    if (h == 0) {
-      ml[wave][lane][0] = rb.m;
-      ml[wave][lane][1] = l;
-    }
+    few_finish<T, DV, NW>(a, rb.o, rb.m, rb.l, smem, FK::kWave, ml, s, kvh, whole, slot);
     __syncthreads();
-    float M = kLowest, L = 0.0f;
+  });
+}
+
+// ---- requests of at most 32 rows over an e4m3 cache ----
+// Codes lie in LDS as they do in memory, in rows of C 16-byte chunks whose order keeps
+// the reads free of bank conflicts: a key's 16 codes by ds_read_b128, 16 rows apart
+// over all banks; of values, 8 keys by 16 columns by ds_read_b64_tr_b8, 16 rows of two
+// chunks over all banks.
+template <int C>
+__device__ __forceinline__ int k8_swz(int r, int c) {
+  if constexpr (C == 8) return c ^ ((r >> 1) & 7);  // (a row's parity moves half the banks)
+  return (c & ~3) | ((c ^ (r >> 2)) & 3);           // rows of 4 or 12: four rows go round the banks
+}
+template <int C>
+__device__ __forceinline__ int v8_swz(int r, int c) {
+  if constexpr (C == 8) return c ^ (((r >> 1) & 3) << 1);
+  return c ^ (((r >> 2) & 1) << 1);
+}
+
+// The loads of 16 keys (values) into LDS, as GranuleOffsets
+template <int C, bool IsK>
+struct GranuleOffsets8 {
+  static constexpr int N = C / 4;
+  uint32_t off[N];
+  __device__ __forceinline__ void set(uint32_t row_bytes, int last_row) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w][lane & 31][0]);
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float mw = ml[w][lane & 31][0], lw = ml[w][lane & 31][1];
-      L += lw == 0.0f ? 0.0f : lw * exp2_fast((mw - M) * a.c);
+    for (int i = 0; i < N; ++i) {
+      const int s = i * 64 + lane, r = s / C, c = s % C;
+      off[i] = (uint32_t)min(r, last_row) * row_bytes + (uint32_t)(IsK ? k8_swz<C>(r, c) : v8_swz<C>(r, c)) * 16u;
     }
-    const float f = rb.m == kLowest ? 0.0f : exp2_fast((rb.m - M) * a.c);
-    float* so = (float*)(smem + wave * FK::kWave) + (lane & 31) * FK::kPitch;
+  }
+  __device__ __forceinline__ void load(const char* base, uint32_t dst) const {
 #pragma unroll
-    for (int b = 0; b < RB::DB; ++b)
+    for (int i = 0; i < N; ++i) load_lds<true>(base, off[i], dst + 1024u * i);
+  }
+};
+// 64 lanes' 4 bytes each from `from` into LDS at dst + 4 * lane; as load_lds
+__device__ __forceinline__ void load_lds4(const char* from, uint32_t dst) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 3\n\t"
+      "global_load_lds_dword %0, off"
+      :
+      : "v"(from), "s"(dst)
+      : "m0");
+}
+
+// A stage holds 32 keys, their values and, in its last 256 bytes, both scales (32 bytes
+// each; the load fills the rest with the same).  128 KB of LDS or more are in flight:
+// eight waves of two stages with 128-wide heads.
+constexpr int few8_waves(int D) { return D == 192 ? 6 : 8; }
+template <int D, int DV>
+struct FewKernel8 {
+  static constexpr int NW = few8_waves(D), S = D == 64 ? 4 : 2;  // waves, stages
+  static constexpr int BN = 32 * NW;
+  static constexpr uint32_t kK = 32 * D, kV = 32 * DV, kStage = kK + kV + 256;
+  static constexpr int kLoads = D / 32 + DV / 32 + 1;  // of a stage
+  static constexpr uint32_t kSums = kFewRows * kFewPitch<DV> * 4;
+  static constexpr uint32_t kWave = S * kStage > kSums ? S * kStage : kSums;
+  static constexpr size_t lds = NW * kWave;
+};
+
+// Bound by memory as paged_few_kernel is, with half its bytes a key.  Keys' scales are
+// applied as their codes become values, in the conversion; values' codes become
+// bfloat16 as they are, which is exact, and their scales go into the weights.  In
+// binary16 the products of weights and scales would leave that type's range: they are
+// split into two bfloat16 terms (2^-17 of a weight is lost, 8 more matrix instructions
+// of 24 a tile, which a memory-bound loop has room for).
+template <typename T, int D, int DV, bool TREE>
+__global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnArgs a) {
+  typedef FewKernel8<D, DV> FK;
+  constexpr int NW = FK::NW, S = FK::S, CK = D / 16, CV = DV / 16;
+  constexpr int kTerms = std::is_same_v<T, F16> ? 2 : 1;
+  typedef RowBlock<T, D, DV, true> RB;
+  typedef Work<kFewRows, FK::BN, true, TREE> W;
+  typedef std::conditional_t<TREE, SeeTree, SeeAll> See;
+  extern __shared__ __align__(128) char smem[];
+  __shared__ float ml[NW][kFewRows][2];
+  __shared__ int tmp[NW + 5], parents[TREE ? kMaxTree : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const uint32_t mine = lds_addr(smem) + wave * FK::kWave;
+  RB rb;
+  // the lane's places in a tile
+  uint32_t ka[D / 32], va[DV / 32];
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *(f32x4*)(so + 32 * b + 2 * i + 4 * h) =
-            f32x4{rb.o[b][i] * f, rb.o[b][i + 1] * f, rb.o[b][i + 2] * f, rb.o[b][i + 3] * f};
-    // a row's joined statistics, in the first wave's slot once every wave has read it
-    __syncthreads();
-    if (wave == 0 && h == 0) {
-      ml[0][lane][0] = M;
-      ml[0][lane][1] = L;
-    }
-    __syncthreads();
-    const int rows = s.n * a.g;
-    for (int i = tid; i < rows * (DV / 8); i += 64 * NW) {
-      const int rr = i / (DV / 8), col = i % (DV / 8) * 8;
-      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+  for (int u = 0; u < D / 32; ++u) ka[u] = (uint32_t)((lane & 31) * CK + k8_swz<CK>(lane & 31, 2 * u + h)) * 16u;
+  {
+    const int j = (lane & 15) >> 1, row = 4 * h + (j & 3) + 8 * (j >> 2);
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float* p = (const float*)(smem + w * FK::kWave) + rr * FK::kPitch + col;
-        x += *(const f32x4*)p;
-        y += *(const f32x4*)(p + 4);
+    for (int b = 0; b < DV / 32; ++b)
+      va[b] = (uint32_t)(row * CV + v8_swz<CV>(row, 2 * b + ((lane >> 4) & 1))) * 16u + (uint32_t)(lane & 1) * 8u;
+  }
+  Keys8<T, D, DV> keys(a);
+  GranuleOffsets8<CK, true> ko;
+  GranuleOffsets8<CV, false> vo;
+  ko.set(a.k_row, kGranule - 1);
+  vo.set(a.v_row, kGranule - 1);
+  each_piece<W, 64 * NW>(a, tmp, a.few_join, [&](int kvh, int r, const Seq& s, int, const Span& sp, int t0, int n, bool whole, int slot) {
+    keys.seq(s, r, kvh);
+    const Order od(sp.lo + t0 * FK::BN + wave * 32, min(sp.hi, sp.lo + (t0 + n) * FK::BN), FK::BN, 32,
+                   TREE ? Span{0, max(s.kv - s.n, 0)} : Span{visible(a, s, s.n - 1).lo, min(visible(a, s, 0).hi, s.kv)});
+    // tile i's two granules and their pages
+    struct Two {
+      int g[2], page[2];
+    };
+    auto where = [&](int i) {
+      Two t;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        t.g[j] = keys.granule(od.key(i) + j * kGranule);
+        t.page[j] = keys.page(t.g[j]);
       }
-      const float m = ml[0][rr][0], lr = ml[0][rr][1];
-      if (whole) {
-        const float inv = lr > 0.0f || !(lr == lr) ? 1.0f / lr : 0.0f;
-        const int token = div_g(a, rr), head = kvh * a.g + rr - token * a.g;
-        *(u32x4*)(a.out + (int64_t)(s.start + token) * a.o_row + (int64_t)head * a.o_head + col * 2) =
-            u32x4{T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv), T::pack(y[0] * inv, y[1] * inv),
-                  T::pack(y[2] * inv, y[3] * inv)};
-        if (a.lse && col == 0)
-          a.lse[(int64_t)(s.start + token) * a.HQ + head] = log_sum<T>(a, m, lr);
-      } else {
-        const int64_t at = (int64_t)slot * kFewRows + rr;
-        *(f32x4*)(a.few_part + at * DV + col) = x;
-        *(f32x4*)(a.few_part + at * DV + col + 4) = y;
-        if (col == 0) {
-          a.few_ml[2 * at] = m;
-          a.few_ml[2 * at + 1] = lr;
+      return t;
+    };
+    auto stage = [&](int i) { return mine + (uint32_t)(i % S) * FK::kStage; };
+    // (rows past the last key repeat it)
+    auto load_k = [&](int i, const Two& t) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const char* p = keys.k + t.page[j] * a.k_page + (int64_t)keys.place(t.g[j]) * a.k_row;
+        const uint32_t dst = stage(i) + j * (kGranule * D);
+        if (t.g[j] + kGranule <= s.kv) {
+          ko.load(p, dst);
+        } else {
+          GranuleOffsets8<CK, true> o;
+          o.set(a.k_row, s.kv - 1 - t.g[j]);
+          o.load(p, dst);
         }
       }
+      // 16 bytes of each granule's keys' scales, then of its values'
+      const int j = (lane >> 2) & 1, page = j ? t.page[1] : t.page[0], g = keys.place(j ? t.g[1] : t.g[0]) + 4 * (lane & 3);
+      const uint8_t* p = lane & 8 ? keys.vs + page * a.vs_page : keys.ks + page * a.ks_page;
+      load_lds4((const char*)p + g, stage(i) + FK::kK + FK::kV);
+    };
+    auto load_v = [&](int i, const Two& t) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const char* p = keys.v + t.page[j] * a.v_page + (int64_t)keys.place(t.g[j]) * a.v_row;
+        const uint32_t dst = stage(i) + FK::kK + j * (kGranule * DV);
+        if (t.g[j] + kGranule <= s.kv) {
+          vo.load(p, dst);
+        } else {
+          GranuleOffsets8<CV, false> o;
+          o.set(a.v_row, s.kv - 1 - t.g[j]);
+          o.load(p, dst);
+        }
+      }
+    };
+    Two ahead;  // of tile i + S, looked up while tile i is taken
+    if (od.n > 0) {
+      Two t[S];
+#pragma unroll
+      for (int i = 0; i < S; ++i) t[i] = where(min(i, od.n - 1));
+      ahead = where(min(S, od.n - 1));
+#pragma unroll
+      for (int i = 0; i < S; ++i)
+        if (i < od.n) {
+          load_k(i, t[i]);
+          load_v(i, t[i]);
+        }
     }
+    const Row row = row_of(a, s, lane & 31);
+    rb.load_q(q_row(a, s, row, kvh));
+    rb.clear();
+    See see{};
+    if constexpr (TREE) see.set(a, s, row.valid ? row.token : -1, lds_addr(parents));
+    const int top = min(row.see.hi, s.kv);
+    auto tile = [&](int i, bool masked) {
+      // the loads of the tiles behind this one, up to S - 1 of them
+      if (i + S <= od.n)
+        wait_loads<(S - 1) * FK::kLoads>();
+      else
+        wait_loads<0>();
+      const uint32_t kt = stage(i), sc = kt + FK::kK + FK::kV;
+      const float scale = scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + (lane & 31)));
+      uint32_t vs[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vs[j] = *(const MOEQ_LDS uint32_t*)(uintptr_t)(sc + 32 + 8 * j + 4 * h);
+      f32x16 x[1];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[0][j] = 0.0f;
+#pragma unroll
+      for (int u = 0; u < D / 32; ++u) {
+        u32x4 lo, hi;
+        decode16<T>(lds_read16(kt + ka[u]), scale, lo, hi);
+        x[0] = T::mma(lo, rb.q[2 * u], x[0]);
+        x[0] = T::mma(hi, rb.q[2 * u + 1], x[0]);
+      }
+      const bool more = i + S < od.n;
+      // the stage's keys and scales are read: the next ones may take their place
+      wait_lds();
+      if (more) load_k(i + S, ahead);
+      if (masked) {
+        RB::mask(x[0], od.key(i), row.see.lo, top);
+        if constexpr (TREE) RB::mask_bits(x[0], see.window(od.key(i)));
+      }
+      rb.rescale(RB::template largest<1>(x), a.c);
+      uint32_t p[kTerms][8];
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) {
+        float w[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          w[e] = exp2_fast(fmaf(x[0][j + e], a.c, rb.neg_mc));
+          rb.l += w[e];
+          // (times 0 whatever the scale of a key that does not exist)
+          w[e] = __builtin_amdgcn_ldexpf(w[e], (int)(vs[j / 4] >> (8 * ((j + e) % 4)) & 255u) - 127);
+        }
+        p[0][j / 2] = Bf16::pack(w[0], w[1]);
+        if constexpr (kTerms == 2)
+          p[1][j / 2] = Bf16::pack(w[0] - Bf16::low(p[0][j / 2]), w[1] - Bf16::high(p[0][j / 2]));
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int b = 0; b < DV / 32; ++b) {
+          const u32x2 c = lds_read_tr8(kt + FK::kK + va[b] + (16 * t) * DV);
+          const u32x4 v = {Bf16::codes<false>(c.x, 1.0f), Bf16::codes<true>(c.x, 1.0f), Bf16::codes<false>(c.y, 1.0f),
+                           Bf16::codes<true>(c.y, 1.0f)};
+#pragma unroll
+          for (int k = 0; k < kTerms; ++k)
+            rb.o[b] = Bf16::mma(v, u32x4{p[k][4 * t], p[k][4 * t + 1], p[k][4 * t + 2], p[k][4 * t + 3]}, rb.o[b]);
+        }
+      wait_lds();
+      if (more) load_v(i + S, ahead);
+      ahead = where(min(i + S + 1, od.n - 1));
+    };
+    for (int i = 0; i < od.masked; ++i) tile(i, true);
+    if (od.masked > 0 && !rb.finite())
+      rb.redo(a.c, row.see.lo, top, od.masked, 32, s.kv, keys, [&](int i) { return od.key(i); }, see);
+    for (int i = od.masked; i < od.n; ++i) tile(i, false);
+    few_finish<T, DV, NW>(a, rb.o, rb.m, rb.l, smem, FK::kWave, ml, s, kvh, whole, slot);
     __syncthreads();
   });
 }
@@ -987,11 +1234,18 @@ hipError_t launch_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipS
     // workgroup takes its four tiles in about the time of the join's launch.
     a.whole = a.max_kv <= 512;
     hipError_t e;
-    {
+    if constexpr (E4M3) {
+      typedef FewKernel8<d.value, DV> FK;
+      static std::atomic<uint64_t> done{0};
+      auto kernel = paged_few8_kernel<T, d.value, DV, TREE>;
+      if ((e = raise_lds_limit((const void*)kernel, done, FK::lds)) != hipSuccess) return e;
+      kernel<<<kFewGroups, 64 * FK::NW, FK::lds, s>>>(a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else {
       constexpr int NW = d.value == 192 ? 3 : 4;  // 160 KB of LDS
       typedef FewKernel<T, d.value, DV, NW> FK;
       static std::atomic<uint64_t> done{0};
-      auto kernel = paged_few_kernel<T, d.value, DV, NW, E4M3, TREE>;
+      auto kernel = paged_few_kernel<T, d.value, DV, NW, TREE>;
       if ((e = raise_lds_limit((const void*)kernel, done, FK::lds)) != hipSuccess) return e;
       kernel<<<kFewGroups, 64 * NW, FK::lds, s>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
