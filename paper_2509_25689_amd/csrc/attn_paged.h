@@ -915,7 +915,7 @@ struct FewKernel8 {
   static constexpr int NW = few8_waves(D), S = D == 64 ? 4 : 2;  // waves, stages
   static constexpr int BN = 32 * NW;
   static constexpr uint32_t kK = 32 * D, kV = 32 * DV, kStage = kK + kV + 256;
-  static constexpr int kLoads = D / 32 + DV / 32 + 1;  // of a stage
+  static constexpr int kLoadsV = DV / 32, kLoads = D / 32 + 1 + kLoadsV;  // of a stage
   static constexpr uint32_t kSums = kFewRows * kFewPitch<DV> * 4;
   static constexpr uint32_t kWave = S * kStage > kSums ? S * kStage : kSums;
   static constexpr size_t lds = NW * kWave;
@@ -962,50 +962,46 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
                    TREE ? Span{0, max(s.kv - s.n, 0)} : Span{visible(a, s, s.n - 1).lo, min(visible(a, s, 0).hi, s.kv)});
     // tile i's two granules and their pages
     struct Two {
-      int g[2], page[2];
+      int g0, g1, page0, page1;
     };
     auto where = [&](int i) {
-      Two t;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        t.g[j] = keys.granule(od.key(i) + j * kGranule);
-        t.page[j] = keys.page(t.g[j]);
-      }
-      return t;
+      const int key = od.key(i), g0 = keys.granule(key), g1 = keys.granule(key + kGranule);
+      return Two{g0, g1, keys.page(g0), keys.page(g1)};
     };
     auto stage = [&](int i) { return mine + (uint32_t)(i % S) * FK::kStage; };
     // (rows past the last key repeat it)
-    auto load_k = [&](int i, const Two& t) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const char* p = keys.k + t.page[j] * a.k_page + (int64_t)keys.place(t.g[j]) * a.k_row;
-        const uint32_t dst = stage(i) + j * (kGranule * D);
-        if (t.g[j] + kGranule <= s.kv) {
-          ko.load(p, dst);
-        } else {
-          GranuleOffsets8<CK, true> o;
-          o.set(a.k_row, s.kv - 1 - t.g[j]);
-          o.load(p, dst);
-        }
+    auto granule_k = [&](int g, int page, uint32_t dst) {
+      const char* p = keys.k + page * a.k_page + (int64_t)keys.place(g) * a.k_row;
+      if (g + kGranule <= s.kv) {
+        ko.load(p, dst);
+      } else {
+        GranuleOffsets8<CK, true> o;
+        o.set(a.k_row, s.kv - 1 - g);
+        o.load(p, dst);
       }
+    };
+    auto granule_v = [&](int g, int page, uint32_t dst) {
+      const char* p = keys.v + page * a.v_page + (int64_t)keys.place(g) * a.v_row;
+      if (g + kGranule <= s.kv) {
+        vo.load(p, dst);
+      } else {
+        GranuleOffsets8<CV, false> o;
+        o.set(a.v_row, s.kv - 1 - g);
+        o.load(p, dst);
+      }
+    };
+    auto load_k = [&](int i, const Two& t) {
+      granule_k(t.g0, t.page0, stage(i));
+      granule_k(t.g1, t.page1, stage(i) + kGranule * D);
       // 16 bytes of each granule's keys' scales, then of its values'
-      const int j = (lane >> 2) & 1, page = j ? t.page[1] : t.page[0], g = keys.place(j ? t.g[1] : t.g[0]) + 4 * (lane & 3);
-      const uint8_t* p = lane & 8 ? keys.vs + page * a.vs_page : keys.ks + page * a.ks_page;
-      load_lds4((const char*)p + g, stage(i) + FK::kK + FK::kV);
+      const uint8_t *k0 = keys.ks + t.page0 * a.ks_page + keys.place(t.g0), *k1 = keys.ks + t.page1 * a.ks_page + keys.place(t.g1),
+                    *v0 = keys.vs + t.page0 * a.vs_page + keys.place(t.g0), *v1 = keys.vs + t.page1 * a.vs_page + keys.place(t.g1);
+      const uint8_t *k = lane & 4 ? k1 : k0, *v = lane & 4 ? v1 : v0;
+      load_lds4((const char*)(lane & 8 ? v : k) + 4 * (lane & 3), stage(i) + FK::kK + FK::kV);
     };
     auto load_v = [&](int i, const Two& t) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const char* p = keys.v + t.page[j] * a.v_page + (int64_t)keys.place(t.g[j]) * a.v_row;
-        const uint32_t dst = stage(i) + FK::kK + j * (kGranule * DV);
-        if (t.g[j] + kGranule <= s.kv) {
-          vo.load(p, dst);
-        } else {
-          GranuleOffsets8<CV, false> o;
-          o.set(a.v_row, s.kv - 1 - t.g[j]);
-          o.load(p, dst);
-        }
-      }
+      granule_v(t.g0, t.page0, stage(i) + FK::kK);
+      granule_v(t.g1, t.page1, stage(i) + FK::kK + kGranule * DV);
     };
     Two ahead;  // of tile i + S, looked up while tile i is taken
     if (od.n > 0) {
@@ -1023,15 +1019,20 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
     const Row row = row_of(a, s, lane & 31);
     rb.load_q(q_row(a, s, row, kvh));
     rb.clear();
+    // (waited for here, and not at their first use: that lies in the loop, whose loads in
+    // flight would be waited for with them every time)
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) asm volatile("" : "+v"(rb.q[t]));
     See see{};
     if constexpr (TREE) see.set(a, s, row.valid ? row.token : -1, lds_addr(parents));
     const int top = min(row.see.hi, s.kv);
     auto tile = [&](int i, bool masked) {
-      // the loads of the tiles behind this one, up to S - 1 of them
+      // The keys are there when this many loads behind them are not: the values, and
+      // the next S - 1 tiles' (at the end, where there are fewer, of none).
       if (i + S <= od.n)
-        wait_loads<(S - 1) * FK::kLoads>();
+        wait_loads<FK::kLoadsV + (S - 1) * FK::kLoads>();
       else
-        wait_loads<0>();
+        wait_loads<FK::kLoadsV>();
       const uint32_t kt = stage(i), sc = kt + FK::kK + FK::kV;
       const float scale = scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + (lane & 31)));
       uint32_t vs[4];
@@ -1071,6 +1072,13 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
         if constexpr (kTerms == 2)
           p[1][j / 2] = Bf16::pack(w[0] - Bf16::low(p[0][j / 2]), w[1] - Bf16::high(p[0][j / 2]));
       }
+      // the values
+      if (more)
+        wait_loads<S * FK::kLoads - FK::kLoadsV>();
+      else if (i + S == od.n)
+        wait_loads<(S - 1) * FK::kLoads>();
+      else
+        wait_loads<0>();
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
