@@ -234,6 +234,12 @@ struct RowBlock {
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[s] = row ? *gptr((const u32x4*)(row + q_chunk(s, h) * 16)) : u32x4{0, 0, 0, 0};
   }
+  // Waits for the queries.  Left to the compiler that is at their first use, in the loop
+  // over the keys, where it would wait for that loop's loads in flight every time.
+  __device__ __forceinline__ void wait_q() {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));
+  }
   // the 8 dims that half h of the wave holds for step s
   static __device__ __forceinline__ int q_chunk(int s, int h) { return CODES ? 4 * (s >> 1) + 2 * h + (s & 1) : 2 * s + h; }
 

@@ -85,10 +85,9 @@ struct Keys8 {
     table = a.table + (int64_t)r * a.table_stride;
   }
   __device__ __forceinline__ int granule(int key) const { return min(key, (kv - 1) & ~(kGranule - 1)); }
-  __device__ __forceinline__ int page(int g) const {
-    const int b = cload(table, g >> a.page_shift);
-    return (uint32_t)b < (uint32_t)a.n_pages ? b : 0;
-  }
+  __device__ __forceinline__ int page(int g) const { return valid(entry(g)); }
+  __device__ __forceinline__ int entry(int g) const { return cload(table, g >> a.page_shift); }
+  __device__ __forceinline__ int valid(int b) const { return (uint32_t)b < (uint32_t)a.n_pages ? b : 0; }
   __device__ __forceinline__ int place(int key) const { return key & ((1 << a.page_shift) - 1); }
   template <int DIM, bool IsK>
   __device__ __forceinline__ void load(const char* p, uint32_t row_bytes, const uint8_t* sc, int g, uint32_t dst) const {
@@ -826,6 +825,7 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
     const Row row = row_of(a, s, lane & 31);
     rb.load_q(q_row(a, s, row, kvh));
     rb.clear();
+    rb.wait_q();
     See see{};
     if constexpr (TREE) see.set(a, s, row.valid ? row.token : -1, lds_addr(parents));
     const int top = min(row.see.hi, s.kv);
@@ -960,19 +960,21 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
     keys.seq(s, r, kvh);
     const Order od(sp.lo + t0 * FK::BN + wave * 32, min(sp.hi, sp.lo + (t0 + n) * FK::BN), FK::BN, 32,
                    TREE ? Span{0, max(s.kv - s.n, 0)} : Span{visible(a, s, s.n - 1).lo, min(visible(a, s, 0).hi, s.kv)});
-    // tile i's two granules and their pages
+    // A tile's two granules and the table's entries for them, which are looked up one
+    // tile before they are checked and used: a read waited for at once is a few hundred
+    // cycles of every tile.
     struct Two {
       int g0, g1, page0, page1;
     };
-    auto where = [&](int i) {
-      const int key = od.key(i), g0 = keys.granule(key), g1 = keys.granule(key + kGranule);
-      return Two{g0, g1, keys.page(g0), keys.page(g1)};
+    auto where = [&](int key) {
+      const int g0 = keys.granule(key), g1 = keys.granule(key + kGranule);
+      return Two{g0, g1, keys.entry(g0), keys.entry(g1)};
     };
     auto stage = [&](int i) { return mine + (uint32_t)(i % S) * FK::kStage; };
-    // (rows past the last key repeat it)
-    auto granule_k = [&](int g, int page, uint32_t dst) {
-      const char* p = keys.k + page * a.k_page + (int64_t)keys.place(g) * a.k_row;
-      if (g + kGranule <= s.kv) {
+    // (rows past the last key repeat it: not in tiles without a mask, FULL)
+    auto granule_k = [&](int g, int page, uint32_t dst, auto full) {
+      const char* p = keys.k + page * a.k_page + (uint64_t)(uint32_t)keys.place(g) * a.k_row;
+      if (full.value || g + kGranule <= s.kv) {
         ko.load(p, dst);
       } else {
         GranuleOffsets8<CK, true> o;
@@ -980,9 +982,9 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
         o.load(p, dst);
       }
     };
-    auto granule_v = [&](int g, int page, uint32_t dst) {
-      const char* p = keys.v + page * a.v_page + (int64_t)keys.place(g) * a.v_row;
-      if (g + kGranule <= s.kv) {
+    auto granule_v = [&](int g, int page, uint32_t dst, auto full) {
+      const char* p = keys.v + page * a.v_page + (uint64_t)(uint32_t)keys.place(g) * a.v_row;
+      if (full.value || g + kGranule <= s.kv) {
         vo.load(p, dst);
       } else {
         GranuleOffsets8<CV, false> o;
@@ -990,50 +992,51 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
         o.load(p, dst);
       }
     };
-    auto load_k = [&](int i, const Two& t) {
-      granule_k(t.g0, t.page0, stage(i));
-      granule_k(t.g1, t.page1, stage(i) + kGranule * D);
-      // 16 bytes of each granule's keys' scales, then of its values'
-      const uint8_t *k0 = keys.ks + t.page0 * a.ks_page + keys.place(t.g0), *k1 = keys.ks + t.page1 * a.ks_page + keys.place(t.g1),
-                    *v0 = keys.vs + t.page0 * a.vs_page + keys.place(t.g0), *v1 = keys.vs + t.page1 * a.vs_page + keys.place(t.g1);
-      const uint8_t *k = lane & 4 ? k1 : k0, *v = lane & 4 ? v1 : v0;
-      load_lds4((const char*)(lane & 8 ? v : k) + 4 * (lane & 3), stage(i) + FK::kK + FK::kV);
+    // a lane's dword of the scales: 16 bytes of each granule's keys, then of its values
+    const char* scales = (const char*)(lane & 8 ? keys.vs : keys.ks) + 4 * (lane & 3);
+    const int64_t scale_page = lane & 8 ? a.vs_page : a.ks_page;
+    auto load_k = [&](uint32_t st, const Two& t, auto full) {
+      const int page0 = keys.valid(t.page0), page1 = keys.valid(t.page1);
+      granule_k(t.g0, page0, st, full);
+      granule_k(t.g1, page1, st + kGranule * D, full);
+      load_lds4(scales + (lane & 4 ? page1 : page0) * scale_page + (lane & 4 ? keys.place(t.g1) : keys.place(t.g0)),
+                st + FK::kK + FK::kV);
     };
-    auto load_v = [&](int i, const Two& t) {
-      granule_v(t.g0, t.page0, stage(i) + FK::kK);
-      granule_v(t.g1, t.page1, stage(i) + FK::kK + kGranule * DV);
+    auto load_v = [&](uint32_t st, const Two& t, auto full) {
+      granule_v(t.g0, keys.valid(t.page0), st + FK::kK, full);
+      granule_v(t.g1, keys.valid(t.page1), st + FK::kK + kGranule * DV, full);
     };
-    Two ahead;  // of tile i + S, looked up while tile i is taken
+    constexpr std::false_type kAny{};
+    constexpr std::true_type kFull{};
+    Two ahead{};  // of tile i + S, looked up while tile i - 1 is taken
     if (od.n > 0) {
       Two t[S];
 #pragma unroll
-      for (int i = 0; i < S; ++i) t[i] = where(min(i, od.n - 1));
-      ahead = where(min(S, od.n - 1));
+      for (int i = 0; i < S; ++i) t[i] = where(od.key(min(i, od.n - 1)));
+      ahead = where(od.key(min(S, od.n - 1)));
 #pragma unroll
       for (int i = 0; i < S; ++i)
         if (i < od.n) {
-          load_k(i, t[i]);
-          load_v(i, t[i]);
+          load_k(stage(i), t[i], kAny);
+          load_v(stage(i), t[i], kAny);
         }
     }
     const Row row = row_of(a, s, lane & 31);
     rb.load_q(q_row(a, s, row, kvh));
     rb.clear();
-    // (waited for here, and not at their first use: that lies in the loop, whose loads in
-    // flight would be waited for with them every time)
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t) asm volatile("" : "+v"(rb.q[t]));
+    rb.wait_q();
     See see{};
     if constexpr (TREE) see.set(a, s, row.valid ? row.token : -1, lds_addr(parents));
     const int top = min(row.see.hi, s.kv);
-    auto tile = [&](int i, bool masked) {
+    // tile i, in stage st; the tile after those in flight begins at key `next`
+    auto tile = [&](int i, uint32_t kt, int next, auto full) {
       // The keys are there when this many loads behind them are not: the values, and
       // the next S - 1 tiles' (at the end, where there are fewer, of none).
       if (i + S <= od.n)
         wait_loads<FK::kLoadsV + (S - 1) * FK::kLoads>();
       else
         wait_loads<FK::kLoadsV>();
-      const uint32_t kt = stage(i), sc = kt + FK::kK + FK::kV;
+      const uint32_t sc = kt + FK::kK + FK::kV;
       const float scale = scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + (lane & 31)));
       uint32_t vs[4];
 #pragma unroll
@@ -1049,10 +1052,12 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
         x[0] = T::mma(hi, rb.q[2 * u + 1], x[0]);
       }
       const bool more = i + S < od.n;
+      const Two now = ahead;
+      ahead = where(next);
       // the stage's keys and scales are read: the next ones may take their place
       wait_lds();
-      if (more) load_k(i + S, ahead);
-      if (masked) {
+      if (more) load_k(kt, now, full);
+      if constexpr (!full.value) {
         RB::mask(x[0], od.key(i), row.see.lo, top);
         if constexpr (TREE) RB::mask_bits(x[0], see.window(od.key(i)));
       }
@@ -1091,13 +1096,21 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
             rb.o[b] = Bf16::mma(v, u32x4{p[k][4 * t], p[k][4 * t + 1], p[k][4 * t + 2], p[k][4 * t + 3]}, rb.o[b]);
         }
       wait_lds();
-      if (more) load_v(i + S, ahead);
-      ahead = where(min(i + S + 1, od.n - 1));
+      if (more) load_v(kt, now, full);
     };
-    for (int i = 0; i < od.masked; ++i) tile(i, true);
+    int i = 0;
+    uint32_t st = 0;
+    for (; i < od.masked; ++i) {
+      tile(i, mine + st, od.key(min(i + S + 1, od.n - 1)), kAny);
+      st = st == (S - 1) * FK::kStage ? 0 : st + FK::kStage;
+    }
     if (od.masked > 0 && !rb.finite())
       rb.redo(a.c, row.see.lo, top, od.masked, 32, s.kv, keys, [&](int i) { return od.key(i); }, see);
-    for (int i = od.masked; i < od.n; ++i) tile(i, false);
+    // (the others lie one after another; beyond the last one nothing is loaded)
+    for (int key = od.key(i) + (S + 1) * FK::BN, last = od.key(max(od.n - 1, 0)); i < od.n; ++i, key += FK::BN) {
+      tile(i, mine + st, min(key, last), kFull);
+      st = st == (S - 1) * FK::kStage ? 0 : st + FK::kStage;
+    }
     few_finish<T, DV, NW>(a, rb.o, rb.m, rb.l, smem, FK::kWave, ml, s, kvh, whole, slot);
     __syncthreads();
   });
