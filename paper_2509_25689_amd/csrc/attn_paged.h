@@ -1041,13 +1041,19 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
       uint32_t vs[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) vs[j] = *(const MOEQ_LDS uint32_t*)(uintptr_t)(sc + 32 + 8 * j + 4 * h);
+      // all of a tile's reads at once (left to the compiler, each into the same registers
+      // and waited for)
+      u32x4 codes[D / 32];
+#pragma unroll
+      for (int u = 0; u < D / 32; ++u) codes[u] = lds_read16(kt + ka[u]);
+      __builtin_amdgcn_sched_barrier(0);
       f32x16 x[1];
 #pragma unroll
       for (int j = 0; j < 16; ++j) x[0][j] = 0.0f;
 #pragma unroll
       for (int u = 0; u < D / 32; ++u) {
         u32x4 lo, hi;
-        decode16<T>(lds_read16(kt + ka[u]), scale, lo, hi);
+        decode16<T>(codes[u], scale, lo, hi);
         x[0] = T::mma(lo, rb.q[2 * u], x[0]);
         x[0] = T::mma(hi, rb.q[2 * u + 1], x[0]);
       }
@@ -1062,6 +1068,19 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
         if constexpr (TREE) RB::mask_bits(x[0], see.window(od.key(i)));
       }
       rb.rescale(RB::template largest<1>(x), a.c);
+      // the values
+      if (more)
+        wait_loads<S * FK::kLoads - FK::kLoadsV>();
+      else if (i + S == od.n)
+        wait_loads<(S - 1) * FK::kLoads>();
+      else
+        wait_loads<0>();
+      u32x2 values[2][DV / 32];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int b = 0; b < DV / 32; ++b) values[t][b] = lds_read_tr8(kt + FK::kK + va[b] + (16 * t) * DV);
+      __builtin_amdgcn_sched_barrier(0);
       uint32_t p[kTerms][8];
 #pragma unroll
       for (int j = 0; j < 16; j += 2) {
@@ -1077,18 +1096,11 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
         if constexpr (kTerms == 2)
           p[1][j / 2] = Bf16::pack(w[0] - Bf16::low(p[0][j / 2]), w[1] - Bf16::high(p[0][j / 2]));
       }
-      // the values
-      if (more)
-        wait_loads<S * FK::kLoads - FK::kLoadsV>();
-      else if (i + S == od.n)
-        wait_loads<(S - 1) * FK::kLoads>();
-      else
-        wait_loads<0>();
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int b = 0; b < DV / 32; ++b) {
-          const u32x2 c = lds_read_tr8(kt + FK::kK + va[b] + (16 * t) * DV);
+          const u32x2 c = values[t][b];
           const u32x4 v = {Bf16::codes<false>(c.x, 1.0f), Bf16::codes<true>(c.x, 1.0f), Bf16::codes<false>(c.y, 1.0f),
                            Bf16::codes<true>(c.y, 1.0f)};
 #pragma unroll
