@@ -49,6 +49,7 @@ struct AttnArgs {
   uint32_t g_mul, g_shift;  // division by g
   int32_t HQ, HK, g, n_seqs, T, causal, window;
   float scale, c;  // c = scale * log2(e)
+  int32_t few_rows;  // a request of at most these rows goes to the few-rows kernel
   int32_t whole;  // segments are not cut: the run that holds a segment's first unit takes it
   int32_t n_slots, heads_together;
   const uint8_t *ks, *vs;  // an e4m3 cache's scales
@@ -64,10 +65,10 @@ struct PagedLayout {
 PagedLayout paged_layout(int DV, bool tiles);
 
 hipError_t launch_attn_prompt(AttnArgs a, int dtype, int D, hipStream_t s);
-hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipStream_t s);
-hipError_t launch_attn_tree(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipStream_t s);
-hipError_t launch_attn_e4m3(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipStream_t s);
-hipError_t launch_attn_e4m3_tree(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipStream_t s);
+hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws, hipStream_t s);
+hipError_t launch_attn_tree(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws, hipStream_t s);
+hipError_t launch_attn_e4m3(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws, hipStream_t s);
+hipError_t launch_attn_e4m3_tree(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws, hipStream_t s);
 
 struct PlanArgs {
   const int32_t *ctx, *add;

@@ -1,5 +1,5 @@
 // Attention over packed prompts, and over a paged cache of 16-bit values.
-#include "attn_paged.h"
+#include "attn_launch.h"
 
 namespace moeq {
 
@@ -118,8 +118,8 @@ PagedLayout paged_layout(int DV, bool tiles) {
   return l;
 }
 
-hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipStream_t s) {
-  return launch_paged<false, false>(a, dtype, D, tiles, ws, s);
+hipError_t launch_attn_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws, hipStream_t s) {
+  return launch_paged<false, false>(a, dtype, D, max_rows, ws, s);
 }
 
 }  // namespace moeq

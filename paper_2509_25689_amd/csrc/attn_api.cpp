@@ -302,7 +302,7 @@ moeq_status attn_over_cache(const moeq_attn* a, const moeq_rows* q, const moeq_k
   g.n_seqs = n_requests;
   g.T = n_tokens;
   const auto launch = scales ? tree ? launch_attn_e4m3_tree : launch_attn_e4m3 : tree ? launch_attn_tree : launch_attn_paged;
-  return done(launch(g, a->dtype, a->head_dim, (int64_t)max_new * g.g > kFewRows, (char*)workspace, (hipStream_t)stream),
+  return done(launch(g, a->dtype, a->head_dim, (int64_t)max_new * g.g, (char*)workspace, (hipStream_t)stream),
               "paged attention launch");
 }
 

@@ -39,6 +39,10 @@ struct Bf16 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
                                                    0, 0);
   }
+  static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+  }
   // the two e4m3 codes in a dword's low (high) half times a power of two
   template <bool HIGH>
   static __device__ __forceinline__ uint32_t codes(uint32_t v, float scale) {
@@ -61,6 +65,10 @@ struct F16 {
   static __device__ __forceinline__ float high(uint32_t v) { return (float)__builtin_bit_cast(f16x2, v)[1]; }
   static __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                  0);
+  }
+  static __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
                                                   0);
   }
   template <bool HIGH>
@@ -178,6 +186,18 @@ __device__ __forceinline__ float max_halves(float v) {
 }
 __device__ __forceinline__ float sum_halves(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// the same over the four lanes 16 apart
+__device__ __forceinline__ float max_quarters(float v) {
+  v = max_halves(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_quarters(float v) {
+  v = sum_halves(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
@@ -354,6 +374,16 @@ struct RowBlock {
         o[b] = T::mma(u32x4{x.x, x.y, y.x, y.y}, pb, o[b]);
       }
     }
+  }
+
+  // the lane's share of its row's sums times f
+  __device__ __forceinline__ void store(float* p, float f) const {
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4*)(p + 32 * b + 2 * i + 4 * h) = f32x4{o[b][i] * f, o[b][i + 1] * f, o[b][i + 2] * f, o[b][i + 3] * f};
   }
 
   // A key that a row does not see has weight 0, but 0 times an infinity or NaN

@@ -1,0 +1,79 @@
+// The launches of attention over a paged cache, for each kind of cache and of mask.
+#pragma once
+
+#include "attn_codes.h"
+#include "attn_paged.h"
+
+namespace moeq {
+
+namespace {
+
+constexpr int kPromptWaves = 4;
+
+// The launches of attention over the cache; max_rows: at least the most of a request
+template <bool E4M3, bool TREE>
+hipError_t launch_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws, hipStream_t s) {
+  const bool tiles = max_rows > kFewRows;
+  return by_type(dtype, D, [&](auto t, auto d, auto dv) -> hipError_t {
+    typedef decltype(t) T;
+    constexpr int DV = dv.value;
+    const PagedLayout l = paged_layout(DV, tiles);
+    a.few_join = (PagedJoin*)(ws + l.few_join);
+    a.few_ml = (float*)(ws + l.few_ml);
+    a.few_part = (float*)(ws + l.few_part);
+    a.tile_join = (PagedJoin*)(ws + l.tile_join);
+    a.tile_ml = (float*)(ws + l.tile_ml);
+    a.tile_part = (float*)(ws + l.tile_part);
+    // Where no request can have more than 512 keys a segment is not cut: a
+    // workgroup takes its four tiles in about the time of the join's launch.
+    a.whole = a.max_kv <= 512;
+    // Which requests the few-rows kernel takes: those of up to 32 rows.  Over codes those
+    // of up to 16 where no other is there, or where the others go to tiles: 48 requests
+    // of 7 rows @@.  A step of trees larger than that is left to the tiles whole: a small
+    // tree among them costs less there than two more launches.
+    a.few_rows = TREE && tiles ? 0 : E4M3 && a.g <= 16 && (tiles || max_rows <= 16) ? 16 : kFewRows;
+    hipError_t e = hipSuccess;
+    if (a.few_rows == 0) {
+    } else if constexpr (E4M3) {
+      auto launch = [&](auto rows) -> hipError_t {
+        typedef FewKernel8<d.value, DV, rows.value> FK;
+        static std::atomic<uint64_t> done{0};
+        auto kernel = paged_few8_kernel<T, d.value, DV, rows.value, TREE>;
+        const hipError_t e = raise_lds_limit((const void*)kernel, done, FK::lds);
+        if (e != hipSuccess) return e;
+        kernel<<<kFewGroups, 64 * FK::NW, FK::lds, s>>>(a);
+        return hipGetLastError();
+      };
+      e = a.few_rows == 16 ? launch(std::integral_constant<int, 16>()) : launch(std::integral_constant<int, 32>());
+    } else {
+      constexpr int NW = d.value == 192 ? 3 : 4;  // 160 KB of LDS
+      typedef FewKernel<T, d.value, DV, NW> FK;
+      static std::atomic<uint64_t> done{0};
+      auto kernel = paged_few_kernel<T, d.value, DV, NW, TREE>;
+      if ((e = raise_lds_limit((const void*)kernel, done, FK::lds)) != hipSuccess) return e;
+      kernel<<<kFewGroups, 64 * NW, FK::lds, s>>>(a);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+    if (tiles) {
+      constexpr int NW = kPromptWaves;
+      typedef TileKernel<T, d.value, DV, NW, true, E4M3, TREE> TK;
+      static std::atomic<uint64_t> done{0};
+      auto kernel = paged_tile_kernel<T, d.value, DV, NW, E4M3, TREE>;
+      if ((e = raise_lds_limit((const void*)kernel, done, TK::lds)) != hipSuccess) return e;
+      kernel<<<kTileGroups, 64 * NW, TK::lds, s>>>(a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (!a.whole) {
+        tile_join_kernel<T, DV, NW><<<kTileGroups, 64 * NW, 0, s>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+    }
+    if (a.whole || a.few_rows == 0) return hipSuccess;
+    few_join_kernel<T, DV><<<dim3(kFewGroups, kFewRows / 4), 256, 0, s>>>(a);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace
+
+}  // namespace moeq

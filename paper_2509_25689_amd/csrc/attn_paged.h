@@ -481,11 +481,11 @@ struct Work {
   static __device__ __forceinline__ int runs_before(int n, int u) {
     return n < kRuns ? u : (int)(((uint64_t)(uint32_t)u * kRuns + n - 1) / (uint32_t)n);
   }
-  // requests of at most 32 rows go to the few-rows kernel, the others to tiles
+  // requests of at most few_rows (32, or less) go to the few-rows kernel, the others to tiles
   static __device__ __forceinline__ int row_tiles(const AttnArgs& a, const Seq& s) {
     const int rows = TREE && s.n > kMaxTree ? 0 : s.n * a.g;  // (larger trees are left out)
-    if constexpr (FEW) return rows > 0 && rows <= kFewRows ? 1 : 0;
-    return rows > kFewRows ? (rows + BM - 1) / BM : 0;
+    if constexpr (FEW) return rows > 0 && rows <= a.few_rows ? 1 : 0;
+    return rows > a.few_rows ? (rows + BM - 1) / BM : 0;
   }
   static __device__ __forceinline__ Span span(const AttnArgs& a, const Seq& s, int qt) {
     const int rows = s.n * a.g, row0 = qt * BM, last = min(row0 + BM, rows) - 1;
@@ -682,40 +682,34 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
 template <int DV>
 constexpr int kFewPitch = DV + 4;
 
-// Joins the waves' sums of a piece's rows (o, m and each lane's half of l) and writes
-// the rows, or the piece's part of them.  smem: wave_bytes for each wave, kFewRows rows
-// at least, read and written by its wave alone so far; the caller waits before the
+// Joins the waves' sums of a piece's rows and writes the rows, or the piece's part of
+// them.  The lane's row is lane % ROWS, m and l its maximum and sum; store(p, f) writes
+// the lane's share of the row's sums times f to p.  smem: wave_bytes for each wave, ROWS
+// rows at least, read and written by its wave alone so far; the caller waits before the
 // next piece.
-template <typename T, int DV, int NW>
-__device__ __forceinline__ void few_finish(const AttnArgs& a, const f32x16 (&o)[DV / 32], float m_own, float l_half,
-                                           char* smem, uint32_t wave_bytes, float (&ml)[NW][kFewRows][2], const Seq& s,
-                                           int kvh, bool whole, int slot) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-  const float l = sum_halves(l_half);
-  if (h == 0) {
+template <typename T, int DV, int NW, int ROWS, typename F>
+__device__ __forceinline__ void few_finish(const AttnArgs& a, F store, float m_own, float l, char* smem,
+                                           uint32_t wave_bytes, float (&ml)[NW][kFewRows][2], const Seq& s, int kvh,
+                                           bool whole, int slot) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (lane < ROWS) {
     ml[wave][lane][0] = m_own;
     ml[wave][lane][1] = l;
   }
   __syncthreads();
   float M = kLowest, L = 0.0f;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w][lane & 31][0]);
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w][lane & (ROWS - 1)][0]);
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
-    const float mw = ml[w][lane & 31][0], lw = ml[w][lane & 31][1];
+    const float mw = ml[w][lane & (ROWS - 1)][0], lw = ml[w][lane & (ROWS - 1)][1];
     L += lw == 0.0f ? 0.0f : lw * exp2_fast((mw - M) * a.c);
   }
   const float f = m_own == kLowest ? 0.0f : exp2_fast((m_own - M) * a.c);
-  float* so = (float*)(smem + wave * wave_bytes) + (lane & 31) * kFewPitch<DV>;
-#pragma unroll
-  for (int b = 0; b < DV / 32; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4)
-      *(f32x4*)(so + 32 * b + 2 * i + 4 * h) =
-          f32x4{o[b][i] * f, o[b][i + 1] * f, o[b][i + 2] * f, o[b][i + 3] * f};
+  store((float*)(smem + wave * wave_bytes) + (lane & (ROWS - 1)) * kFewPitch<DV>, f);
   // a row's joined statistics, in the first wave's slot once every wave has read it
   __syncthreads();
-  if (wave == 0 && h == 0) {
+  if (wave == 0 && lane < ROWS) {
     ml[0][lane][0] = M;
     ml[0][lane][1] = L;
   }
@@ -856,274 +850,8 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
     if (od.masked > 0 && !rb.finite())
       rb.redo(a.c, row.see.lo, top, od.masked, 32, s.kv, keys, [&](int i) { return od.key(i); }, see);
     for (int i = od.masked; i < od.n; ++i) tile(i, false);
-    few_finish<T, DV, NW>(a, rb.o, rb.m, rb.l, smem, FK::kWave, ml, s, kvh, whole, slot);
-    __syncthreads();
-  });
-}
-
-// ---- requests of at most 32 rows over an e4m3 cache ----
-// Codes lie in LDS as they do in memory, in rows of C 16-byte chunks whose order keeps
-// the reads free of bank conflicts: a key's 16 codes by ds_read_b128, 16 rows apart
-// over all banks; of values, 8 keys by 16 columns by ds_read_b64_tr_b8, 16 rows of two
-// chunks over all banks.
-template <int C>
-__device__ __forceinline__ int k8_swz(int r, int c) {
-  if constexpr (C == 8) return c ^ ((r >> 1) & 7);  // (a row's parity moves half the banks)
-  return (c & ~3) | ((c ^ (r >> 2)) & 3);           // rows of 4 or 12: four rows go round the banks
-}
-template <int C>
-__device__ __forceinline__ int v8_swz(int r, int c) {
-  if constexpr (C == 8) return c ^ (((r >> 1) & 3) << 1);
-  return c ^ (((r >> 2) & 1) << 1);
-}
-
-// The loads of 16 keys (values) into LDS, as GranuleOffsets
-template <int C, bool IsK>
-struct GranuleOffsets8 {
-  static constexpr int N = C / 4;
-  uint32_t off[N];
-  __device__ __forceinline__ void set(uint32_t row_bytes, int last_row) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int s = i * 64 + lane, r = s / C, c = s % C;
-      off[i] = (uint32_t)min(r, last_row) * row_bytes + (uint32_t)(IsK ? k8_swz<C>(r, c) : v8_swz<C>(r, c)) * 16u;
-    }
-  }
-  __device__ __forceinline__ void load(const char* base, uint32_t dst) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) load_lds<true>(base, off[i], dst + 1024u * i);
-  }
-};
-// 64 lanes' 4 bytes each from `from` into LDS at dst + 4 * lane; as load_lds
-__device__ __forceinline__ void load_lds4(const char* from, uint32_t dst) {
-  asm volatile(
-      "s_mov_b32 m0, %1\n\t"
-      "s_nop 3\n\t"
-      "global_load_lds_dword %0, off"
-      :
-      : "v"(from), "s"(dst)
-      : "m0");
-}
-
-// A stage holds 32 keys, their values and, in its last 256 bytes, both scales (32 bytes
-// each; the load fills the rest with the same).  128 KB of LDS or more are in flight:
-// eight waves of two stages with 128-wide heads.
-constexpr int few8_waves(int D) { return D == 192 ? 6 : 8; }
-template <int D, int DV>
-struct FewKernel8 {
-  static constexpr int NW = few8_waves(D), S = D == 64 ? 4 : 2;  // waves, stages
-  static constexpr int BN = 32 * NW;
-  static constexpr uint32_t kK = 32 * D, kV = 32 * DV, kStage = kK + kV + 256;
-  static constexpr int kLoadsV = DV / 32, kLoads = D / 32 + 1 + kLoadsV;  // of a stage
-  static constexpr uint32_t kSums = kFewRows * kFewPitch<DV> * 4;
-  static constexpr uint32_t kWave = S * kStage > kSums ? S * kStage : kSums;
-  static constexpr size_t lds = NW * kWave;
-};
-
-// Bound by memory as paged_few_kernel is, with half its bytes a key.  Keys' scales are
-// applied as their codes become values, in the conversion; values' codes become
-// bfloat16 as they are, which is exact, and their scales go into the weights.  In
-// binary16 the products of weights and scales would leave that type's range: they are
-// split into two bfloat16 terms (2^-17 of a weight is lost, 8 more matrix instructions
-// of 24 a tile, which a memory-bound loop has room for).
-template <typename T, int D, int DV, bool TREE>
-__global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnArgs a) {
-  typedef FewKernel8<D, DV> FK;
-  constexpr int NW = FK::NW, S = FK::S, CK = D / 16, CV = DV / 16;
-  constexpr int kTerms = std::is_same_v<T, F16> ? 2 : 1;
-  typedef RowBlock<T, D, DV, true> RB;
-  typedef Work<kFewRows, FK::BN, true, TREE> W;
-  typedef std::conditional_t<TREE, SeeTree, SeeAll> See;
-  extern __shared__ __align__(128) char smem[];
-  __shared__ float ml[NW][kFewRows][2];
-  __shared__ int tmp[NW + 5], parents[TREE ? kMaxTree : 1];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const uint32_t mine = lds_addr(smem) + wave * FK::kWave;
-  RB rb;
-  // the lane's places in a tile
-  uint32_t ka[D / 32], va[DV / 32];
-#pragma unroll
-  for (int u = 0; u < D / 32; ++u) ka[u] = (uint32_t)((lane & 31) * CK + k8_swz<CK>(lane & 31, 2 * u + h)) * 16u;
-  {
-    const int j = (lane & 15) >> 1, row = 4 * h + (j & 3) + 8 * (j >> 2);
-#pragma unroll
-    for (int b = 0; b < DV / 32; ++b)
-      va[b] = (uint32_t)(row * CV + v8_swz<CV>(row, 2 * b + ((lane >> 4) & 1))) * 16u + (uint32_t)(lane & 1) * 8u;
-  }
-  Keys8<T, D, DV> keys(a);
-  GranuleOffsets8<CK, true> ko;
-  GranuleOffsets8<CV, false> vo;
-  ko.set(a.k_row, kGranule - 1);
-  vo.set(a.v_row, kGranule - 1);
-  each_piece<W, 64 * NW>(a, tmp, a.few_join, [&](int kvh, int r, const Seq& s, int, const Span& sp, int t0, int n, bool whole, int slot) {
-    keys.seq(s, r, kvh);
-    const Order od(sp.lo + t0 * FK::BN + wave * 32, min(sp.hi, sp.lo + (t0 + n) * FK::BN), FK::BN, 32,
-                   TREE ? Span{0, max(s.kv - s.n, 0)} : Span{visible(a, s, s.n - 1).lo, min(visible(a, s, 0).hi, s.kv)});
-    // A tile's two granules and the table's entries for them, which are looked up one
-    // tile before they are checked and used: a read waited for at once is a few hundred
-    // cycles of every tile.
-    struct Two {
-      int g0, g1, page0, page1;
-    };
-    auto where = [&](int key) {
-      const int g0 = keys.granule(key), g1 = keys.granule(key + kGranule);
-      return Two{g0, g1, keys.entry(g0), keys.entry(g1)};
-    };
-    auto stage = [&](int i) { return mine + (uint32_t)(i % S) * FK::kStage; };
-    // (rows past the last key repeat it: not in tiles without a mask, FULL)
-    auto granule_k = [&](int g, int page, uint32_t dst, auto full) {
-      const char* p = keys.k + page * a.k_page + (uint64_t)(uint32_t)keys.place(g) * a.k_row;
-      if (full.value || g + kGranule <= s.kv) {
-        ko.load(p, dst);
-      } else {
-        GranuleOffsets8<CK, true> o;
-        o.set(a.k_row, s.kv - 1 - g);
-        o.load(p, dst);
-      }
-    };
-    auto granule_v = [&](int g, int page, uint32_t dst, auto full) {
-      const char* p = keys.v + page * a.v_page + (uint64_t)(uint32_t)keys.place(g) * a.v_row;
-      if (full.value || g + kGranule <= s.kv) {
-        vo.load(p, dst);
-      } else {
-        GranuleOffsets8<CV, false> o;
-        o.set(a.v_row, s.kv - 1 - g);
-        o.load(p, dst);
-      }
-    };
-    // a lane's dword of the scales: 16 bytes of each granule's keys, then of its values
-    const char* scales = (const char*)(lane & 8 ? keys.vs : keys.ks) + 4 * (lane & 3);
-    const int64_t scale_page = lane & 8 ? a.vs_page : a.ks_page;
-    auto load_k = [&](uint32_t st, const Two& t, auto full) {
-      const int page0 = keys.valid(t.page0), page1 = keys.valid(t.page1);
-      granule_k(t.g0, page0, st, full);
-      granule_k(t.g1, page1, st + kGranule * D, full);
-      load_lds4(scales + (lane & 4 ? page1 : page0) * scale_page + (lane & 4 ? keys.place(t.g1) : keys.place(t.g0)),
-                st + FK::kK + FK::kV);
-    };
-    auto load_v = [&](uint32_t st, const Two& t, auto full) {
-      granule_v(t.g0, keys.valid(t.page0), st + FK::kK, full);
-      granule_v(t.g1, keys.valid(t.page1), st + FK::kK + kGranule * DV, full);
-    };
-    constexpr std::false_type kAny{};
-    constexpr std::true_type kFull{};
-    Two ahead{};  // of tile i + S, looked up while tile i - 1 is taken
-    if (od.n > 0) {
-      Two t[S];
-#pragma unroll
-      for (int i = 0; i < S; ++i) t[i] = where(od.key(min(i, od.n - 1)));
-      ahead = where(od.key(min(S, od.n - 1)));
-#pragma unroll
-      for (int i = 0; i < S; ++i)
-        if (i < od.n) {
-          load_k(stage(i), t[i], kAny);
-          load_v(stage(i), t[i], kAny);
-        }
-    }
-    const Row row = row_of(a, s, lane & 31);
-    rb.load_q(q_row(a, s, row, kvh));
-    rb.clear();
-    rb.wait_q();
-    See see{};
-    if constexpr (TREE) see.set(a, s, row.valid ? row.token : -1, lds_addr(parents));
-    const int top = min(row.see.hi, s.kv);
-    // tile i, in stage st; the tile after those in flight begins at key `next`
-    auto tile = [&](int i, uint32_t kt, int next, auto full) {
-      // The keys are there when this many loads behind them are not: the values, and
-      // the next S - 1 tiles' (at the end, where there are fewer, of none).
-      if (i + S <= od.n)
-        wait_loads<FK::kLoadsV + (S - 1) * FK::kLoads>();
-      else
-        wait_loads<FK::kLoadsV>();
-      const uint32_t sc = kt + FK::kK + FK::kV;
-      const float scale = scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + (lane & 31)));
-      uint32_t vs[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) vs[j] = *(const MOEQ_LDS uint32_t*)(uintptr_t)(sc + 32 + 8 * j + 4 * h);
-      // all of a tile's reads at once (left to the compiler, each into the same registers
-      // and waited for)
-      u32x4 codes[D / 32];
-#pragma unroll
-      for (int u = 0; u < D / 32; ++u) codes[u] = lds_read16(kt + ka[u]);
-      __builtin_amdgcn_sched_barrier(0);
-      f32x16 x[1];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) x[0][j] = 0.0f;
-#pragma unroll
-      for (int u = 0; u < D / 32; ++u) {
-        u32x4 lo, hi;
-        decode16<T>(codes[u], scale, lo, hi);
-        x[0] = T::mma(lo, rb.q[2 * u], x[0]);
-        x[0] = T::mma(hi, rb.q[2 * u + 1], x[0]);
-      }
-      const bool more = i + S < od.n;
-      const Two now = ahead;
-      ahead = where(next);
-      // the stage's keys and scales are read: the next ones may take their place
-      wait_lds();
-      if (more) load_k(kt, now, full);
-      if constexpr (!full.value) {
-        RB::mask(x[0], od.key(i), row.see.lo, top);
-        if constexpr (TREE) RB::mask_bits(x[0], see.window(od.key(i)));
-      }
-      rb.rescale(RB::template largest<1>(x), a.c);
-      // the values
-      if (more)
-        wait_loads<S * FK::kLoads - FK::kLoadsV>();
-      else if (i + S == od.n)
-        wait_loads<(S - 1) * FK::kLoads>();
-      else
-        wait_loads<0>();
-      u32x2 values[2][DV / 32];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int b = 0; b < DV / 32; ++b) values[t][b] = lds_read_tr8(kt + FK::kK + va[b] + (16 * t) * DV);
-      __builtin_amdgcn_sched_barrier(0);
-      uint32_t p[kTerms][8];
-#pragma unroll
-      for (int j = 0; j < 16; j += 2) {
-        float w[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          w[e] = exp2_fast(fmaf(x[0][j + e], a.c, rb.neg_mc));
-          rb.l += w[e];
-          // (times 0 whatever the scale of a key that does not exist)
-          w[e] = __builtin_amdgcn_ldexpf(w[e], (int)(vs[j / 4] >> (8 * ((j + e) % 4)) & 255u) - 127);
-        }
-        p[0][j / 2] = Bf16::pack(w[0], w[1]);
-        if constexpr (kTerms == 2)
-          p[1][j / 2] = Bf16::pack(w[0] - Bf16::low(p[0][j / 2]), w[1] - Bf16::high(p[0][j / 2]));
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int b = 0; b < DV / 32; ++b) {
-          const u32x2 c = values[t][b];
-          const u32x4 v = {Bf16::codes<false>(c.x, 1.0f), Bf16::codes<true>(c.x, 1.0f), Bf16::codes<false>(c.y, 1.0f),
-                           Bf16::codes<true>(c.y, 1.0f)};
-#pragma unroll
-          for (int k = 0; k < kTerms; ++k)
-            rb.o[b] = Bf16::mma(v, u32x4{p[k][4 * t], p[k][4 * t + 1], p[k][4 * t + 2], p[k][4 * t + 3]}, rb.o[b]);
-        }
-      wait_lds();
-      if (more) load_v(kt, now, full);
-    };
-    int i = 0;
-    uint32_t st = 0;
-    for (; i < od.masked; ++i) {
-      tile(i, mine + st, od.key(min(i + S + 1, od.n - 1)), kAny);
-      st = st == (S - 1) * FK::kStage ? 0 : st + FK::kStage;
-    }
-    if (od.masked > 0 && !rb.finite())
-      rb.redo(a.c, row.see.lo, top, od.masked, 32, s.kv, keys, [&](int i) { return od.key(i); }, see);
-    // (the others lie one after another; beyond the last one nothing is loaded)
-    for (int key = od.key(i) + (S + 1) * FK::BN, last = od.key(max(od.n - 1, 0)); i < od.n; ++i, key += FK::BN) {
-      tile(i, mine + st, min(key, last), kFull);
-      st = st == (S - 1) * FK::kStage ? 0 : st + FK::kStage;
-    }
-    few_finish<T, DV, NW>(a, rb.o, rb.m, rb.l, smem, FK::kWave, ml, s, kvh, whole, slot);
+    few_finish<T, DV, NW, kFewRows>(a, [&](float* p, float f) { rb.store(p, f); }, rb.m, sum_halves(rb.l), smem, FK::kWave,
+                                    ml, s, kvh, whole, slot);
     __syncthreads();
   });
 }
@@ -1246,60 +974,6 @@ hipError_t by_type(int dtype, int D, F f) {
   if (D == 64) return f(F16(), std::integral_constant<int, 64>(), std::integral_constant<int, 64>());
   if (D == 128) return f(F16(), std::integral_constant<int, 128>(), std::integral_constant<int, 128>());
   return f(F16(), std::integral_constant<int, 192>(), std::integral_constant<int, 128>());
-}
-
-constexpr int kPromptWaves = 4;
-
-// The launches of attention over the cache
-template <bool E4M3, bool TREE>
-hipError_t launch_paged(AttnArgs a, int dtype, int D, bool tiles, char* ws, hipStream_t s) {
-  return by_type(dtype, D, [&](auto t, auto d, auto dv) -> hipError_t {
-    typedef decltype(t) T;
-    constexpr int DV = dv.value;
-    const PagedLayout l = paged_layout(DV, tiles);
-    a.few_join = (PagedJoin*)(ws + l.few_join);
-    a.few_ml = (float*)(ws + l.few_ml);
-    a.few_part = (float*)(ws + l.few_part);
-    a.tile_join = (PagedJoin*)(ws + l.tile_join);
-    a.tile_ml = (float*)(ws + l.tile_ml);
-    a.tile_part = (float*)(ws + l.tile_part);
-    // Where no request can have more than 512 keys a segment is not cut: a
-    // workgroup takes its four tiles in about the time of the join's launch.
-    a.whole = a.max_kv <= 512;
-    hipError_t e;
-    if constexpr (E4M3) {
-      typedef FewKernel8<d.value, DV> FK;
-      static std::atomic<uint64_t> done{0};
-      auto kernel = paged_few8_kernel<T, d.value, DV, TREE>;
-      if ((e = raise_lds_limit((const void*)kernel, done, FK::lds)) != hipSuccess) return e;
-      kernel<<<kFewGroups, 64 * FK::NW, FK::lds, s>>>(a);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    } else {
-      constexpr int NW = d.value == 192 ? 3 : 4;  // 160 KB of LDS
-      typedef FewKernel<T, d.value, DV, NW> FK;
-      static std::atomic<uint64_t> done{0};
-      auto kernel = paged_few_kernel<T, d.value, DV, NW, TREE>;
-      if ((e = raise_lds_limit((const void*)kernel, done, FK::lds)) != hipSuccess) return e;
-      kernel<<<kFewGroups, 64 * NW, FK::lds, s>>>(a);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (tiles) {
-      constexpr int NW = kPromptWaves;
-      typedef TileKernel<T, d.value, DV, NW, true, E4M3, TREE> TK;
-      static std::atomic<uint64_t> done{0};
-      auto kernel = paged_tile_kernel<T, d.value, DV, NW, E4M3, TREE>;
-      if ((e = raise_lds_limit((const void*)kernel, done, TK::lds)) != hipSuccess) return e;
-      kernel<<<kTileGroups, 64 * NW, TK::lds, s>>>(a);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-      if (!a.whole) {
-        tile_join_kernel<T, DV, NW><<<kTileGroups, 64 * NW, 0, s>>>(a);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-      }
-    }
-    if (a.whole) return hipSuccess;
-    few_join_kernel<T, DV><<<dim3(kFewGroups, kFewRows / 4), 256, 0, s>>>(a);
-    return hipGetLastError();
-  });
 }
 
 }  // namespace
