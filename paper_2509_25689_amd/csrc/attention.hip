@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(AttnArgs a) {
     ad.set();
     rb.clear();
   });
-  store_out<T, DV>(a, rb.o, rb.m, sum_halves(rb.l), s, r, kvh);
+  store_out<T>(a, rb.o, rb.m, sum_halves(rb.l), s, r, kvh);
 }
 
 }  // namespace

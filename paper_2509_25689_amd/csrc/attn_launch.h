@@ -64,7 +64,7 @@ hipError_t launch_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws
       kernel<<<kTileGroups, 64 * NW, TK::lds, s>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       if (!a.whole) {
-        tile_join_kernel<T, DV, NW><<<kTileGroups, 64 * NW, 0, s>>>(a);
+        tile_join_kernel<T, DV, NW><<<dim3(kTileGroups, DV / 32), 64 * NW, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
       }
     }

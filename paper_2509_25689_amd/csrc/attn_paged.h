@@ -226,9 +226,10 @@ __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
   return l == 0.0f ? -INFINITY : m * a.scale + __logf(l * unlift);
 }
 
-template <typename T, int DV, int DB>
+// o: the blocks of 32 columns from the b0-th on
+template <typename T, int DB>
 __device__ __forceinline__ void store_out(const AttnArgs& a, const f32x16 (&o)[DB], float m, float l, const Seq& s,
-                                          const Row& r, int kvh) {
+                                          const Row& r, int kvh, int b0 = 0) {
   const int h = (threadIdx.x >> 5) & 1;
   const int head = kvh * a.g + r.head;
   const float inv = l > 0.0f || !(l == l) ? 1.0f / l : 0.0f;
@@ -247,9 +248,9 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, const f32x16 (&o)[D
       }
       const auto u = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
       const auto w = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
-      if (r.valid) *(u32x4*)(row + (32 * b + 16 * t + 8 * h) * 2) = u32x4{u[0], w[0], u[1], w[1]};
+      if (r.valid) *(u32x4*)(row + (32 * (b0 + b) + 16 * t + 8 * h) * 2) = u32x4{u[0], w[0], u[1], w[1]};
     }
-  if (a.lse && r.valid && h == 0)
+  if (a.lse && r.valid && h == 0 && b0 == 0)
     a.lse[(int64_t)(s.start + r.token) * a.HQ + head] = log_sum<T>(a, m, l);
 }
 
@@ -666,7 +667,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
     });
     const float l = sum_halves(rb.l);
     if (whole) {
-      store_out<T, DV>(a, rb.o, rb.m, l, s, row, kvh);
+      store_out<T>(a, rb.o, rb.m, l, s, row, kvh);
     } else {
       f32x4* part = tile_part<DV>(a, slot * NW + wave);
 #pragma unroll
@@ -859,12 +860,25 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
 // The pieces of the segment that run w begins: its own, the next runs' first ones.
 __device__ __forceinline__ int piece_slot(int w, int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); }
 
-// Adds up the pieces of cut segments: of tiled rows, one workgroup a segment,
-// each wave its 32 rows, in the registers' order.  Bound by memory (up to 134 MB of
-// sums): 15 us beside the chunks of four prompts.
+// The run whose segment a join's workgroup takes.  Segments that begin every 32 or 64
+// runs, as those of one request do, would all fall to workgroups of one XCD (b % 8),
+// through whose port their pieces then come: the runs of each eight are turned by
+// their number.
+__device__ __forceinline__ int join_run() {
+  const int base = blockIdx.x & ~7;
+  return base | ((blockIdx.x - (base >> 3) - (base >> 6) - blockIdx.y) & 7);
+}
+
+// Adds up the pieces of cut segments: of tiled rows, workgroup (w, b) the b-th 32
+// columns of a segment, each wave its 32 rows, in the registers' order.  Bound by the
+// reads' latency where few segments are cut into many pieces, so U of them are in
+// flight (one request's tree of 24 tokens over 8192 keys, 16 segments of 32 pieces:
+// 70 us with all columns in one workgroup and a piece at a time, @@); by memory with
+// many (up to 134 MB of sums).
 template <typename T, int DV, int NW>
 __global__ __launch_bounds__(64 * NW) void tile_join_kernel(AttnArgs a) {
-  const int w = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int U = 4;
+  const int w = join_run(), col = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const PagedJoin rec = a.tile_join[w];
   if (rec.parts == 0) return;
   const Seq s{rec.start, rec.n, 0};
@@ -873,33 +887,40 @@ __global__ __launch_bounds__(64 * NW) void tile_join_kernel(AttnArgs a) {
   r.valid = row < rec.n * a.g;
   r.token = div_g(a, row);
   r.head = row - r.token * a.g;
-  f32x16 o[DV / 32];
+  f32x16 o[1];
 #pragma unroll
-  for (int b = 0; b < DV / 32; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[b][i] = 0.0f;
+  for (int i = 0; i < 16; ++i) o[0][i] = 0.0f;
   float M = kLowest, L = 0.0f;
-  for (int i = 0; i < rec.parts; ++i) {
-    const int at = piece_slot(w, i) * NW + wave;
-    const f32x4* part = tile_part<DV>(a, at);
-    const f32x2v ml = *tile_ml(a, at);
-    f32x4 x[DV / 8];
+  for (int i0 = 0; i0 < rec.parts; i0 += U) {
+    f32x2v ml[U];
+    f32x4 x[U][4];
 #pragma unroll
-    for (int j = 0; j < DV / 8; ++j) x[j] = part[j * 64];
-    const float next = fmaxf(M, ml[0]);
-    const float f0 = M == kLowest ? 0.0f : exp2_fast((M - next) * a.c);
-    const float f = ml[0] == kLowest ? 0.0f : exp2_fast((ml[0] - next) * a.c);
+    for (int u = 0; u < U; ++u) {
+      const int at = piece_slot(w, min(i0 + u, rec.parts - 1)) * NW + wave;
+      ml[u] = *tile_ml(a, at);
 #pragma unroll
-    for (int j = 0; j < DV / 8; ++j)
+      for (int j = 0; j < 4; ++j) x[u][j] = tile_part<DV>(a, at)[(4 * col + j) * 64];
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (or each piece's reads are waited for in turn)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float& v = ((float*)&o[j / 4])[4 * (j % 4) + e];
-        v = fmaf(f, x[j][e], f0 * v);
-      }
-    L = fmaf(f, ml[1], f0 * L);
-    M = next;
+    for (int u = 0; u < U; ++u) {
+      const bool there = i0 + u < rec.parts;
+      const float next = fmaxf(M, ml[u][0]);
+      const float f0 = M == kLowest ? 0.0f : exp2_fast((M - next) * a.c);
+      const float f = ml[u][0] == kLowest ? 0.0f : exp2_fast((ml[u][0] - next) * a.c);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = fmaf(f, x[u][j][e], f0 * o[0][4 * j + e]);
+          o[0][4 * j + e] = there ? v : o[0][4 * j + e];
+        }
+      const float l = fmaf(f, ml[u][1], f0 * L);
+      L = there ? l : L;
+      M = there ? next : M;
+    }
   }
-  store_out<T, DV>(a, o, M, L, s, r, rec.kvh);
+  store_out<T>(a, o, M, L, s, r, rec.kvh, col);
 }
 
 // Of single rows: workgroup (w, y), one wave a row, DV / 64 columns a lane.  Bound
@@ -908,7 +929,7 @@ __global__ __launch_bounds__(64 * NW) void tile_join_kernel(AttnArgs a) {
 template <typename T, int DV>
 __global__ __launch_bounds__(256) void few_join_kernel(AttnArgs a) {
   constexpr int NC = DV / 64;
-  const int w = blockIdx.x;
+  const int w = join_run();
   const PagedJoin rec = a.few_join[w];
   if (rec.parts == 0) return;
   const float *part = a.few_part, *ml = a.few_ml;
