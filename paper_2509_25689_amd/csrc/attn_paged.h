@@ -89,26 +89,40 @@ struct Keys8 {
   __device__ __forceinline__ int entry(int g) const { return cload(table, g >> a.page_shift); }
   __device__ __forceinline__ int valid(int b) const { return (uint32_t)b < (uint32_t)a.n_pages ? b : 0; }
   __device__ __forceinline__ int place(int key) const { return key & ((1 << a.page_shift) - 1); }
-  template <int DIM, bool IsK>
-  __device__ __forceinline__ void load(const char* p, uint32_t row_bytes, const uint8_t* sc, int g, uint32_t dst) const {
-    constexpr int C = DIM / 16;  // 16-byte chunks of a row
-    const int lane = threadIdx.x & 63, last = min(kGranule, kv - g) - 1;
-    u32x4 x[C / 4];
-    uint32_t e[C / 4];
+  // A lane's chunks of a granule: 16 codes each, and their rows' scales
+  struct Raw {
+    u32x4 k[D / 64], v[DV / 64];
+    uint32_t ke[D / 64], ve[DV / 64];
+  };
+  template <int C>
+  static __device__ __forceinline__ void fetch(const char* p, uint32_t row_bytes, const uint8_t* sc, int last,
+                                               u32x4 (&x)[C / 4], uint32_t (&e)[C / 4]) {
 #pragma unroll
     for (int i = 0; i < C / 4; ++i) {
-      const int s = i * 64 + lane, r = min(s / C, last), c = s % C;
+      const int s = i * 64 + (threadIdx.x & 63), r = min(s / C, last), c = s % C;
       x[i] = *gptr((const u32x4*)(p + (uint32_t)r * row_bytes + c * 16));
       e[i] = *gptr(sc + r);
     }
-#pragma unroll
-    for (int i = 0; i < C / 4; ++i) {
-      const int s = i * 64 + lane, r = s / C, c = s % C;
-      u32x4 lo, hi;
-      decode16<T>(x[i], scale_of(e[i]), lo, hi);
-      lds_write16(dst + (uint32_t)(r * 2 * C + (IsK ? k_swz<2 * C>(r, 2 * c) : v_swz<2 * C>(r, 2 * c))) * 16u, lo);
-      lds_write16(dst + (uint32_t)(r * 2 * C + (IsK ? k_swz<2 * C>(r, 2 * c + 1) : v_swz<2 * C>(r, 2 * c + 1))) * 16u, hi);
-    }
+  }
+  // granule g's (rows past the last key repeat it)
+  __device__ __forceinline__ void fetch(int g, int page, Raw& raw) const {
+    const int last = min(kGranule, kv - g) - 1;
+    fetch<D / 16>(k + page * a.k_page + (int64_t)place(g) * a.k_row, a.k_row, ks + page * a.ks_page + place(g), last,
+                  raw.k, raw.ke);
+    fetch<DV / 16>(v + page * a.v_page + (int64_t)place(g) * a.v_row, a.v_row, vs + page * a.vs_page + place(g), last,
+                   raw.v, raw.ve);
+  }
+  static constexpr int kChunks = D / 64 + DV / 64;
+  // The i-th chunk's values into LDS, where the granule's keys lie at kd, its values at vd
+  static __device__ __forceinline__ void put(const Raw& raw, int i, uint32_t kd, uint32_t vd) {
+    const bool key = i < D / 64;
+    const int j = key ? i : i - D / 64, C = key ? D / 16 : DV / 16;
+    const int s = j * 64 + (threadIdx.x & 63), r = s / C, c = s % C;
+    u32x4 lo, hi;
+    decode16<T>(key ? raw.k[j] : raw.v[j], scale_of(key ? raw.ke[j] : raw.ve[j]), lo, hi);
+    const uint32_t dst = (key ? kd : vd) + (uint32_t)(r * 2 * C) * 16u;
+    lds_write16(dst + (uint32_t)(key ? k_swz<D / 8>(r, 2 * c) : v_swz<DV / 8>(r, 2 * c)) * 16u, lo);
+    lds_write16(dst + (uint32_t)(key ? k_swz<D / 8>(r, 2 * c + 1) : v_swz<DV / 8>(r, 2 * c + 1)) * 16u, hi);
   }
   __device__ __forceinline__ Row8<T> key_row(int key) const {
     const int b = page(key & ~(kGranule - 1)), i = place(key);
@@ -117,12 +131,6 @@ struct Keys8 {
   __device__ __forceinline__ Row8<T> value_row(int key) const {
     const int b = page(key & ~(kGranule - 1)), i = place(key);
     return Row8<T>{v + b * a.v_page + (int64_t)i * a.v_row, scale_of(vs[b * a.vs_page + i])};
-  }
-  __device__ __forceinline__ void load_k(int g, int page, uint32_t dst) const {
-    load<D, true>(k + page * a.k_page + (int64_t)place(g) * a.k_row, a.k_row, ks + page * a.ks_page + place(g), g, dst);
-  }
-  __device__ __forceinline__ void load_v(int g, int page, uint32_t dst) const {
-    load<DV, false>(v + page * a.v_page + (int64_t)place(g) * a.v_row, a.v_row, vs + page * a.vs_page + place(g), g, dst);
   }
 };
 
@@ -337,6 +345,86 @@ struct TileKernel {
   static __device__ __forceinline__ void run(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
                                              const K& keys, const Row& r, const See& see, int lo, int hi, Span all,
                                              F begin) {
+    if constexpr (E4M3)
+      run_codes(a, base, rb, ad, keys, r, see, lo, hi, all, begin);
+    else
+      run_values(a, base, rb, ad, keys, r, see, lo, hi, all, begin);
+  }
+
+  // Codes go through the registers: a tile's are read while the one before it is taken,
+  // decoded between the steps of its scores and written as values to the other stage.
+  // The loads stay in flight across the barrier, which waits for LDS alone.  (The scores
+  // of a tile ahead, as below, do not fit the registers beside the codes.)
+  template <typename F>
+  static __device__ __forceinline__ void run_codes(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
+                                                   const K& keys, const Row& r, const See& see, int lo, int hi, Span all,
+                                                   F begin) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Order od(lo, hi, kTileKeys, kTileKeys, all);
+    const int nt = od.n;
+    typename K::Raw raw;
+    auto granule = [&](int i) { return keys.granule(od.key(i) + wave * kGranule); };
+    auto put = [&](int i, int chunk) {
+      const uint32_t st = base + (i & 1) * kStage;
+      K::put(raw, chunk, st + wave * (kGranule * D * 2), st + kK + wave * (kGranule * DV * 2));
+    };
+    int entry = 0;  // the table's for the tile after the one that is fetched next
+    if (nt > 0) {
+      const int g = granule(0), page = keys.page(g);
+      entry = keys.entry(granule(min(1, nt - 1)));
+      keys.fetch(g, page, raw);
+    }
+    begin();
+    rb.wait_q();
+    auto fetch = [&](int i) {  // tile i, if there is one
+      if (i >= nt) return;
+      keys.fetch(granule(i), keys.valid(entry), raw);
+      entry = keys.entry(granule(min(i + 1, nt - 1)));
+    };
+    if (nt > 0) {
+#pragma unroll
+      for (int c = 0; c < K::kChunks; ++c) put(0, c);
+      fetch(1);
+    }
+    auto tile = [&](int i, auto masked) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+      const uint32_t st = base + (i & 1) * kStage;
+      f32x16 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        s[b] = rb.scores(ad, st + b * 32 * D * 2, [&](int t) {
+          // (past the last tile: what no one reads)
+          const int step = b * RB::KS + t;
+          static_assert(4 * K::kChunks <= 2 * RB::KS, "a step for every chunk");
+          if (step % 4 == 1 && step / 4 < K::kChunks) put(i + 1, step / 4);
+        });
+      fetch(i + 2);
+      if constexpr (masked.value) {
+        const int key = od.key(i), top = min(r.see.hi, keys.kv);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          RB::mask(s[b], key + 32 * b, r.see.lo, top);
+          if constexpr (TREE) RB::mask_bits(s[b], see.window(key + 32 * b));
+        }
+      }
+      rb.rescale(RB::template largest<2>(s), a.c);
+      uint32_t p[2][8];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) rb.weights(s[b], a.c, p[b]);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) rb.values(ad, st + kK + b * 32 * DV * 2, p[b]);
+    };
+    for (int i = 0; i < od.masked; ++i) tile(i, std::true_type());
+    if (od.masked > 0 && !rb.finite())
+      rb.redo(a.c, r.see.lo, min(r.see.hi, keys.kv), od.masked, kTileKeys, hi, keys, [&](int i) { return od.key(i); }, see);
+    for (int i = od.masked; i < nt; ++i) tile(i, std::false_type());
+    stage_barrier();
+  }
+
+  template <typename F>
+  static __device__ __forceinline__ void run_values(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
+                                                    const K& keys, const Row& r, const See& see, int lo, int hi, Span all,
+                                                    F begin) {
     static_assert(NW * kGranule == kTileKeys, "a wave loads one granule of a tile");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Order od(lo, hi, kTileKeys, kTileKeys, all);
@@ -379,84 +467,73 @@ struct TileKernel {
     }
     if (od.masked > 0 && !rb.finite())
       rb.redo(a.c, r.see.lo, min(r.see.hi, keys.kv), od.masked, kTileKeys, hi, keys, [&](int i) { return od.key(i); }, see);
-    if constexpr (E4M3) {
+    // the page of this wave's granule of the i-th tile (at most the last)
+    auto page_of = [&](int i) { return keys.page(od.key(min(i, nt - 1)) + wave * kGranule); };
+    // Loads of tile tk's keys and tile tv's values, in pages pk and pv, both
+    // without a mask (so with no granule that ends early), to the stages of tiles
+    // ik and iv (past the end the last tile's again, where no one reads them), one
+    // at a time between the steps of a product:
+    // issued together, the workgroup's waves wait for each other's (8 loads a
+    // wave 650 of a tile's 2900 cycles).  There are 2 KS steps; every second one
+    // carries a load.
+    auto spread = [&](int tk, int ik, int pk, int tv, int iv, int pv) {
+      const int gk = od.key(tk) + wave * kGranule, gv = od.key(tv) + wave * kGranule;
+      const char* kp = keys.k + keys.row_at(gk, pk, a.k_page, a.k_row);
+      const char* vp = keys.v + keys.row_at(gv, pv, a.v_page, a.v_row);
+      const uint32_t kd = base + (ik & 1) * kStage + wave * (kGranule * D * 2);
+      const uint32_t vd = base + (iv & 1) * kStage + kK + wave * (kGranule * DV * 2);
+      return [=, &keys](int step) {
+        constexpr int NK = GranuleOffsets<D / 8, true, false>::N, NV = GranuleOffsets<DV / 8, false, false>::N;
+        static_assert(2 * (NK + NV) <= 2 * RB::KS, "a step for every load");
+        if (step & 1) return;
+        const int j = step >> 1;
+        if (j < NK)
+          keys.ko.load_one(kp, kd, j);
+        else if (j < NK + NV)
+          keys.vo.load_one(vp, vd, j - NK);
+      };
+    };
+    if constexpr (PAGED && D > 128) {
+      // (the scores of two tiles do not fit the registers beside 192-wide queries
+      // and the pages' state)
+      int page1 = od.masked < nt ? page_of(od.masked + 1) : 0;
       for (int i = od.masked; i < nt; ++i) {
         stage_barrier();
-        if (i + 1 < nt) load(i + 1, true, true);
         f32x16 s[2];
-        scores(i, s, nothing);
+        const int t1 = min(i + 1, nt - 1);
+        scores(i, s, spread(t1, i + 1, page1, t1, i + 1, page1));
+        page1 = page_of(i + 2);
         rb.rescale(RB::template largest<2>(s), a.c);
         finish(i, s);
       }
-    } else {
-      // the page of this wave's granule of the i-th tile (at most the last)
-      auto page_of = [&](int i) { return keys.page(od.key(min(i, nt - 1)) + wave * kGranule); };
-      // Loads of tile tk's keys and tile tv's values, in pages pk and pv, both
-      // without a mask (so with no granule that ends early), to the stages of tiles
-      // ik and iv (past the end the last tile's again, where no one reads them), one
-      // at a time between the steps of a product:
-      // issued together, the workgroup's waves wait for each other's (8 loads a
-      // wave 650 of a tile's 2900 cycles).  There are 2 KS steps; every second one
-      // carries a load.
-      auto spread = [&](int tk, int ik, int pk, int tv, int iv, int pv) {
-        const int gk = od.key(tk) + wave * kGranule, gv = od.key(tv) + wave * kGranule;
-        const char* kp = keys.k + keys.row_at(gk, pk, a.k_page, a.k_row);
-        const char* vp = keys.v + keys.row_at(gv, pv, a.v_page, a.v_row);
-        const uint32_t kd = base + (ik & 1) * kStage + wave * (kGranule * D * 2);
-        const uint32_t vd = base + (iv & 1) * kStage + kK + wave * (kGranule * DV * 2);
-        return [=, &keys](int step) {
-          constexpr int NK = GranuleOffsets<D / 8, true, false>::N, NV = GranuleOffsets<DV / 8, false, false>::N;
-          static_assert(2 * (NK + NV) <= 2 * RB::KS, "a step for every load");
-          if (step & 1) return;
-          const int j = step >> 1;
-          if (j < NK)
-            keys.ko.load_one(kp, kd, j);
-          else if (j < NK + NV)
-            keys.vo.load_one(vp, vd, j - NK);
-        };
+    } else if (od.masked < nt) {
+      // The other tiles, one ahead: the scores of the next tile are formed on the
+      // matrix cores while the vector units take this one's exponentials.
+      int i = od.masked, page1 = page_of(i + 1), page2 = page_of(i + 2);  // of tiles i + 1, i + 2
+      auto step = [&](int i, const f32x16 (&s)[2], f32x16 (&next)[2]) {
+        rb.rescale(RB::template largest<2>(s), a.c);
+        stage_barrier();  // the next tile's keys and this one's values are there
+        scores(i + 1, next, spread(min(i + 2, nt - 1), i + 2, page2, i + 1, i + 1, page1));
+        page1 = page2;
+        page2 = page_of(i + 3);
+        finish(i, s);
       };
-      if constexpr (PAGED && D > 128) {
-        // (the scores of two tiles do not fit the registers beside 192-wide queries
-        // and the pages' state)
-        int page1 = od.masked < nt ? page_of(od.masked + 1) : 0;
-        for (int i = od.masked; i < nt; ++i) {
-          stage_barrier();
-          f32x16 s[2];
-          const int t1 = min(i + 1, nt - 1);
-          scores(i, s, spread(t1, i + 1, page1, t1, i + 1, page1));
-          page1 = page_of(i + 2);
-          rb.rescale(RB::template largest<2>(s), a.c);
-          finish(i, s);
-        }
-      } else if (od.masked < nt) {
-        // The other tiles, one ahead: the scores of the next tile are formed on the
-        // matrix cores while the vector units take this one's exponentials.
-        int i = od.masked, page1 = page_of(i + 1), page2 = page_of(i + 2);  // of tiles i + 1, i + 2
-        auto step = [&](int i, const f32x16 (&s)[2], f32x16 (&next)[2]) {
-          rb.rescale(RB::template largest<2>(s), a.c);
-          stage_barrier();  // the next tile's keys and this one's values are there
-          scores(i + 1, next, spread(min(i + 2, nt - 1), i + 2, page2, i + 1, i + 1, page1));
-          page1 = page2;
-          page2 = page_of(i + 3);
-          finish(i, s);
-        };
-        f32x16 s0[2], s1[2];
-        stage_barrier();
-        if (i + 1 < nt) load(i + 1, true, false);
-        scores(i, s0, nothing);
-        for (; i + 2 < nt; i += 2) {
-          step(i, s0, s1);
-          step(i + 1, s1, s0);
-        }
-        if (i + 1 < nt) {
-          step(i++, s0, s1);
-#pragma unroll
-          for (int b = 0; b < 2; ++b) s0[b] = s1[b];
-        }
-        rb.rescale(RB::template largest<2>(s0), a.c);
-        stage_barrier();
-        finish(i, s0);
+      f32x16 s0[2], s1[2];
+      stage_barrier();
+      if (i + 1 < nt) load(i + 1, true, false);
+      scores(i, s0, nothing);
+      for (; i + 2 < nt; i += 2) {
+        step(i, s0, s1);
+        step(i + 1, s1, s0);
       }
+      if (i + 1 < nt) {
+        step(i++, s0, s1);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s0[b] = s1[b];
+      }
+      rb.rescale(RB::template largest<2>(s0), a.c);
+      stage_barrier();
+      finish(i, s0);
     }
     stage_barrier();
   }
