@@ -130,10 +130,14 @@ struct TrimArgs {
 hipError_t launch_kv_trim(const TrimArgs& a, hipStream_t s);
 
 // What a request's walk leaves to the choice of its last token: the node it ended at,
-// how many of its children were rejected, and the residuals' sums before each.
+// how many of its children were rejected, and the residuals' sums before each, or
+// (without draft rows) their tokens.
 struct VerifyEnd {
-  int32_t node, rejected, first, n;
-  double z[kMaxTree];
+  int32_t node, rejected, first, pad;
+  union {
+    double z[kMaxTree];
+    int32_t gone[kMaxTree];
+  };
 };
 struct VerifyArgs {
   const int32_t *tokens, *parents, *cu;

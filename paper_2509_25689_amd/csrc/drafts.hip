@@ -72,6 +72,7 @@ __device__ __forceinline__ double residual(float p, float q, const double* z, in
 __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
   __shared__ int parent[kMaxTree], token[kMaxTree];
   __shared__ float px[kMaxTree], qx[kMaxTree], u[kMaxTree];
+  __shared__ int n_gone;
   __shared__ double z[kMaxTree], tmp[kThreads / 64];
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int first = min(max(a.cu[r], 0), a.T), n = min(max(a.cu[r + 1], first), a.T) - first;
@@ -85,7 +86,8 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
     }
     return;
   }
-  static_assert(kThreads >= kMaxTree, "a thread a token");
+  static_assert(kThreads == kMaxTree, "a thread a token");
+  if (tid == 0) n_gone = 0;
   if (tid < n) {
     const int p = a.parents[first + tid], x = a.tokens[first + tid];
     const bool child = p >= 0 && p < tid, there = child && (uint32_t)x < (uint32_t)a.V;
@@ -159,44 +161,60 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
     end->node = at;
     end->rejected = rejected;
     end->first = first;
-    end->n = n;
   }
-  if (a.draft && tid < rejected) end->z[tid] = z[tid];
+  if (a.draft) {
+    if (tid < rejected) end->z[tid] = z[tid];
+  } else if (tid < n && tid > at && parent[tid] == at) {
+    // (all its children are rejected: in any order)
+    end->gone[atomicAdd(&n_gone, 1)] = token[tid];
+  }
 }
 
-// The last residual: of chunk `chunk` of the row that a request ended
-// at, this thread's kPer values.  gone, z: LDS.
+// The last residual: of a chunk of the row that a request ended at, this thread's kPer
+// values.  What the walk left is read at once, before it is known what of it counts.
 struct Last {
+  int node, rejected, first;
   double r[kPer];
+  double z;   // with draft rows: the sum before rejection tid
+  int token;  // without: what rejection tid took
+  __device__ __forceinline__ explicit Last(const VerifyArgs& a, int request) {
+    const VerifyEnd* end = a.end + request;
+    z = 0.0;
+    token = -1;
+    if (a.draft)
+      z = end->z[threadIdx.x];
+    else
+      token = end->gone[threadIdx.x];
+    node = end->node;
+    rejected = end->rejected;
+    first = end->first;
+  }
   __device__ __forceinline__ double sum() const {
     double s = 0.0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) s += r[i];
     return s;
   }
-  __device__ __forceinline__ void read(const VerifyArgs& a, const VerifyEnd* end, int chunk, bool whole, int* gone,
-                                       int* n_gone, double* z) {
+  // whole: of the target's row itself.  gone, zs: LDS
+  __device__ __forceinline__ void read(const VerifyArgs& a, int chunk, bool whole, int* gone, int* n_gone, double* zs) {
     const int tid = threadIdx.x, j = chunk * kPart + tid * kPer;
-    const int node = end->node, first = end->first, rejected = whole ? 0 : end->rejected;
+    const int n = whole ? 0 : rejected;
     float p[kPer], q[kPer];
     read_row(a.target + (int64_t)(first + node) * a.target_row, j, a.V, p);
-    if (a.draft && rejected) {
+    if (a.draft && n) {
       read_row(a.draft + (int64_t)(first + node) * a.draft_row, j, a.V, q);
-      if (tid < rejected) z[tid] = end->z[tid];
+      if (tid < n) zs[tid] = z;
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) r[i] = residual(p[i], q[i], z, rejected);
+      for (int i = 0; i < kPer; ++i) r[i] = residual(p[i], q[i], zs, n);
     } else {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) r[i] = p[i];
-      if (rejected) {
-        // the node's children's tokens that lie in this chunk
+      if (n) {
+        // the rejected tokens that lie in this chunk
         if (tid == 0) *n_gone = 0;
         __syncthreads();
-        if (tid < end->n && a.parents[first + tid] == node && tid > node) {
-          const int x = a.tokens[first + tid];
-          if ((uint32_t)x < (uint32_t)a.V && x / kPart == chunk) gone[atomicAdd(n_gone, 1)] = x;
-        }
+        if (tid < n && (uint32_t)token < (uint32_t)a.V && token / kPart == chunk) gone[atomicAdd(n_gone, 1)] = token;
         __syncthreads();
         for (int g = 0; g < *n_gone; ++g)
 #pragma unroll
@@ -211,10 +229,9 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
   __shared__ int gone[kMaxTree], n_gone;
   __shared__ double z[kMaxTree], tmp[kThreads / 64];
   const int chunk = blockIdx.x % a.n_chunks, r = blockIdx.x / a.n_chunks;
-  const VerifyEnd* end = a.end + r;
-  if (end->node < 0) return;
-  Last last;
-  last.read(a, end, chunk, false, gone, &n_gone, z);
+  Last last(a, r);
+  if (last.node < 0) return;
+  last.read(a, chunk, false, gone, &n_gone, z);
   const double s = group_sum(last.sum(), tmp);
   if (threadIdx.x == 0) a.sums[(int64_t)r * a.n_chunks + chunk] = s;
 }
@@ -248,26 +265,22 @@ __device__ __forceinline__ Scan group_scan(double own, double* tmp) {
 // the place in it.
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
   __shared__ int gone[kMaxTree], n_gone, found, some;
-  __shared__ double z[kMaxTree], tmp[kThreads / 64], ahead, sums[kThreads];
+  __shared__ double z[kMaxTree], tmp[kThreads / 64], ahead;
   const int r = blockIdx.x, tid = threadIdx.x;
-  const VerifyEnd* end = a.end + r;
-  if (end->node < 0) return;
+  const int count = a.counts[r];
   const double last = a.last[r];
-  Last row;
+  double chunk_sum = tid < a.n_chunks ? a.sums[(int64_t)r * a.n_chunks + tid] : 0.0;
+  Last row(a, r);
+  if (row.node < 0) return;
   int token = -1;
   for (int whole = 0; whole < 2; ++whole) {  // the residual; where nothing is left of it, the target's row
-    double own = 0.0;  // of chunk tid
-    if (!whole) {
-      if (tid < a.n_chunks) own = a.sums[(int64_t)r * a.n_chunks + tid];
-    } else {
+    if (whole)
       for (int c = 0; c < a.n_chunks; ++c) {
-        row.read(a, end, c, true, gone, &n_gone, z);
+        row.read(a, c, true, gone, &n_gone, z);
         const double s = group_sum(row.sum(), tmp);
-        if (tid == 0) sums[c] = s;
+        if (tid == c) chunk_sum = s;
       }
-      __syncthreads();
-      if (tid < a.n_chunks) own = sums[tid];
-    }
+    const double own = chunk_sum;
     if (tid == 0) found = some = -1;
     const Scan in = group_scan(own, tmp);  // (of chunk tid)
     if (in.all == 0.0) continue;
@@ -285,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
     __syncthreads();
     if (tid == 0) found = some = -1;
     if (c < 0) break;  // (sums below 0 among them)
-    row.read(a, end, c, whole, gone, &n_gone, z);
+    row.read(a, c, whole, gone, &n_gone, z);
     const Scan at = group_scan(row.sum(), tmp);
     double t = ahead + at.before;
     int mine = -1, positive = -1;
@@ -303,7 +316,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
     token = found >= 0 ? found : some;
     break;
   }
-  if (tid == 0) a.out[(int64_t)r * a.width + a.counts[r] - 1] = token;
+  if (tid == 0) a.out[(int64_t)r * a.width + count - 1] = token;
 }
 
 }  // namespace
