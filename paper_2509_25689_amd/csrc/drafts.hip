@@ -261,10 +261,34 @@ __device__ __forceinline__ Scan group_scan(double own, double* tmp) {
   return s;
 }
 
+// Of the threads with first >= 0 the first one's, of those with last >= 0 the last one's
+// (-1: none); tmp: two ints for each wave
+struct Ends {
+  int first, last;
+};
+__device__ __forceinline__ Ends group_ends(int first, int last, int* tmp) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t f = __ballot(first >= 0), l = __ballot(last >= 0);
+  const int own_first = f ? __shfl(first, __builtin_ctzll(f), 64) : -1;
+  const int own_last = l ? __shfl(last, 63 - __builtin_clzll(l), 64) : -1;
+  if (lane == 0) {
+    tmp[2 * wave] = own_first;
+    tmp[2 * wave + 1] = own_last;
+  }
+  __syncthreads();
+  Ends e{-1, -1};
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (e.first < 0) e.first = tmp[2 * w];
+    if (tmp[2 * w + 1] >= 0) e.last = tmp[2 * w + 1];
+  }
+  return e;
+}
+
 // The token that follows: one workgroup a request finds the chunk by the sums, then
-// the place in it.
+// the place in it.  Bound by its chain of two reads and two scans.
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
-  __shared__ int gone[kMaxTree], n_gone, found, some;
+  __shared__ int gone[kMaxTree], n_gone, ends[2][2 * (kThreads / 64)];
   __shared__ double z[kMaxTree], tmp[kThreads / 64], ahead;
   const int r = blockIdx.x, tid = threadIdx.x;
   const int count = a.counts[r];
@@ -280,26 +304,18 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
         const double s = group_sum(row.sum(), tmp);
         if (tid == c) chunk_sum = s;
       }
-    const double own = chunk_sum;
-    if (tid == 0) found = some = -1;
-    const Scan in = group_scan(own, tmp);  // (of chunk tid)
+    const Scan in = group_scan(chunk_sum, tmp);  // (of chunk tid)
     if (in.all == 0.0) continue;
     if (!(in.all > 0.0 && in.all < INFINITY)) break;
     const double goal = last * in.all;
     // the first chunk that passes the goal; the last that holds anything, if rounding leaves none
-    if (own > 0.0) {
-      atomicMax(&some, tid);
-      if (in.before + own > goal) atomicMin((unsigned*)&found, (unsigned)tid);
-    }
-    __syncthreads();
-    const bool passed = found >= 0;
-    const int c = passed ? found : some;
-    if (tid == c) ahead = in.before;
-    __syncthreads();
-    if (tid == 0) found = some = -1;
+    const bool some = chunk_sum > 0.0;
+    const Ends chunk = group_ends(some && in.before + chunk_sum > goal ? tid : -1, some ? tid : -1, ends[0]);
+    const int c = chunk.first >= 0 ? chunk.first : chunk.last;
     if (c < 0) break;  // (sums below 0 among them)
+    if (tid == c) ahead = in.before;
     row.read(a, c, whole, gone, &n_gone, z);
-    const Scan at = group_scan(row.sum(), tmp);
+    const Scan at = group_scan(row.sum(), tmp);  // (whose barriers come before `ahead` is read)
     double t = ahead + at.before;
     int mine = -1, positive = -1;
 #pragma unroll
@@ -310,10 +326,8 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
         if (t > goal && mine < 0) mine = positive;
       }
     }
-    if (passed && mine >= 0) atomicMin((unsigned*)&found, (unsigned)mine);
-    if (positive >= 0) atomicMax(&some, positive);
-    __syncthreads();
-    token = found >= 0 ? found : some;
+    const Ends place = group_ends(chunk.first >= 0 ? mine : -1, positive, ends[1]);
+    token = place.first >= 0 ? place.first : place.last;
     break;
   }
   if (tid == 0) a.out[(int64_t)r * a.width + count - 1] = token;
