@@ -67,51 +67,59 @@ __device__ __forceinline__ double residual(float p, float q, const double* z, in
   return r;
 }
 
-// One workgroup a request: the walk.  Every wave takes the same way; where a sibling
+// The walk of request r by one workgroup, every wave on the same way; where a sibling
 // after a rejected one is tried, the whole workgroup sums the residual.
-__global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
-  __shared__ int parent[kMaxTree], token[kMaxTree];
-  __shared__ float px[kMaxTree], qx[kMaxTree], u[kMaxTree];
-  __shared__ int n_gone;
-  __shared__ double z[kMaxTree], tmp[kThreads / 64];
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+struct WalkShared {
+  int parent[kMaxTree], token[kMaxTree];
+  float px[kMaxTree], qx[kMaxTree], u[kMaxTree];
+  double z[kMaxTree], tmp[kThreads / 64];
+  int n_gone;
+};
+struct Walk {
+  int first, n, node, count, rejected;  // node -1: nothing to keep, or left out
+};
+// write: the path and what follows from it (one workgroup of a request's)
+__device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, WalkShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63;
   const int first = min(max(a.cu[r], 0), a.T), n = min(max(a.cu[r + 1], first), a.T) - first;
   int32_t *path = a.path + (int64_t)r * a.width, *out = a.out + (int64_t)r * a.width;
   VerifyEnd* end = a.end + r;
-  if (n < 1 || n > kMaxTree || n > a.width) {  // nothing to keep, or left out
-    for (int i = tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
-    if (tid == 0) {
-      a.counts[r] = 0;
-      end->node = -1;
+  if (n < 1 || n > kMaxTree || n > a.width) {
+    if (write) {
+      for (int i = tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
+      if (tid == 0) {
+        a.counts[r] = 0;
+        end->node = -1;
+      }
     }
-    return;
+    return Walk{first, 0, -1, 0, 0};
   }
   static_assert(kThreads == kMaxTree, "a thread a token");
-  if (tid == 0) n_gone = 0;
+  if (tid == 0) sh.n_gone = 0;
   if (tid < n) {
     const int p = a.parents[first + tid], x = a.tokens[first + tid];
+    sh.u[tid] = a.uniform[first + tid];
     const bool child = p >= 0 && p < tid, there = child && (uint32_t)x < (uint32_t)a.V;
-    parent[tid] = child ? p : -1;
-    token[tid] = x;
-    px[tid] = there ? a.target[(int64_t)(first + p) * a.target_row + x] : 0.0f;
-    qx[tid] = there && a.draft ? a.draft[(int64_t)(first + p) * a.draft_row + x] : 1.0f;
-    u[tid] = a.uniform[first + tid];
+    sh.parent[tid] = child ? p : -1;
+    sh.token[tid] = x;
+    sh.px[tid] = there ? a.target[(int64_t)(first + p) * a.target_row + x] : 0.0f;
+    sh.qx[tid] = there && a.draft ? a.draft[(int64_t)(first + p) * a.draft_row + x] : 1.0f;
   }
   __syncthreads();
   int at = 0, count = 1, rejected = 0;
-  if (tid == 0) path[0] = 0;
+  if (write && tid == 0) path[0] = 0;
   for (int next = 1; next >= 0;) {  // the children of `at`
     next = -1;
     rejected = 0;
     double total = 1.0;
     for (int c0 = (at + 1) & ~63; c0 < n && next < 0; c0 += 64) {
-      uint64_t some = __ballot(c0 + lane < n && parent[min(c0 + lane, n - 1)] == at);
+      uint64_t some = __ballot(c0 + lane < n && sh.parent[min(c0 + lane, n - 1)] == at);
       while (some) {
         const int c = c0 + __builtin_ctzll(some);
         some &= some - 1;
-        const int x = token[c];
+        const int x = sh.token[c];
         const bool there = (uint32_t)x < (uint32_t)a.V;
-        double rx = px[c];
+        double rx = sh.px[c];
         if (a.draft) {
           if (rejected > 0) {
             // (siblings after a rejected one alone take a pass over the row)
@@ -122,23 +130,23 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
               read_row(p, j, a.V, pv);
               read_row(q, j, a.V, qv);
 #pragma unroll
-              for (int i = 0; i < kPer; ++i) sum += residual(pv[i], qv[i], z, rejected);
+              for (int i = 0; i < kPer; ++i) sum += residual(pv[i], qv[i], sh.z, rejected);
             }
-            total = group_sum(sum, tmp);
-            rx = residual(px[c], qx[c], z, rejected);
+            total = group_sum(sum, sh.tmp);
+            rx = residual(sh.px[c], sh.qx[c], sh.z, rejected);
           }
         } else if (there && rejected > 0) {
           // what an earlier sibling of the same token took
           for (int b = at + 1; b < c; ++b)
-            if (parent[b] == at && token[b] == x) rx = 0.0;
+            if (sh.parent[b] == at && sh.token[b] == x) rx = 0.0;
         }
-        if (there && (double)u[c] * (double)qx[c] * total < rx) {
+        if (there && (double)sh.u[c] * (double)sh.qx[c] * total < rx) {
           next = c;
           break;
         }
         if (a.draft) {
           __syncthreads();
-          if (tid == 0) z[rejected] = total;
+          if (tid == 0) sh.z[rejected] = total;
           __syncthreads();
         } else {
           total -= rx;
@@ -148,26 +156,35 @@ __global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
     }
     if (next >= 0) {
       at = next;
-      if (tid == 0) {
+      if (write && tid == 0) {
         path[count] = at;
-        out[count - 1] = token[at];
+        out[count - 1] = sh.token[at];
       }
       ++count;
     }
   }
-  for (int i = count + tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
-  if (tid == 0) {
-    a.counts[r] = count;
-    end->node = at;
-    end->rejected = rejected;
-    end->first = first;
+  if (write) {
+    for (int i = count + tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
+    if (tid == 0) {
+      a.counts[r] = count;
+      end->node = at;
+      end->rejected = rejected;
+      end->first = first;
+    }
+    if (a.draft) {
+      if (tid < rejected) end->z[tid] = sh.z[tid];
+    } else if (tid < n && sh.parent[tid] == at) {
+      // (all its children are rejected: in any order)
+      end->gone[atomicAdd(&sh.n_gone, 1)] = sh.token[tid];
+    }
   }
-  if (a.draft) {
-    if (tid < rejected) end->z[tid] = z[tid];
-  } else if (tid < n && tid > at && parent[tid] == at) {
-    // (all its children are rejected: in any order)
-    end->gone[atomicAdd(&n_gone, 1)] = token[tid];
-  }
+  return Walk{first, n, at, count, rejected};
+}
+
+// One workgroup a request
+__global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
+  __shared__ WalkShared sh;
+  walk(a, blockIdx.x, true, sh);
 }
 
 // The last residual: of a chunk of the row that a request ended at, this thread's kPer
@@ -177,7 +194,11 @@ struct Last {
   double r[kPer];
   double z;   // with draft rows: the sum before rejection tid
   int token;  // without: what rejection tid took
-  __device__ __forceinline__ explicit Last(const VerifyArgs& a, int request) {
+  __device__ __forceinline__ Last(const VerifyArgs& a, const Walk& w, const WalkShared& sh)
+      : node(w.node), rejected(w.rejected), first(w.first), z(0.0) {  // (without draft rows)
+    token = (int)threadIdx.x < w.n && sh.parent[threadIdx.x] == w.node ? sh.token[threadIdx.x] : -1;
+  }
+  __device__ __forceinline__ Last(const VerifyArgs& a, int request) {
     const VerifyEnd* end = a.end + request;
     z = 0.0;
     token = -1;
@@ -188,6 +209,7 @@ struct Last {
     node = end->node;
     rejected = end->rejected;
     first = end->first;
+    if ((int)threadIdx.x >= rejected) token = -1;
   }
   __device__ __forceinline__ double sum() const {
     double s = 0.0;
@@ -214,7 +236,7 @@ struct Last {
         // the rejected tokens that lie in this chunk
         if (tid == 0) *n_gone = 0;
         __syncthreads();
-        if (tid < n && (uint32_t)token < (uint32_t)a.V && token / kPart == chunk) gone[atomicAdd(n_gone, 1)] = token;
+        if ((uint32_t)token < (uint32_t)a.V && token / kPart == chunk) gone[atomicAdd(n_gone, 1)] = token;
         __syncthreads();
         for (int g = 0; g < *n_gone; ++g)
 #pragma unroll
@@ -224,16 +246,28 @@ struct Last {
   }
 };
 
-// The residual's sum over one chunk of the row: workgroup (chunk, request)
+// The residual's sum over one chunk of the row: workgroup (chunk, request).  WALK:
+// without draft rows a walk is two reads and a few steps in LDS, and each of a request's
+// workgroups takes it: for one request of 24 tokens that is @@ a call instead of 12.6
+// with a launch of its own.
+template <bool WALK>
 __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
   __shared__ int gone[kMaxTree], n_gone;
-  __shared__ double z[kMaxTree], tmp[kThreads / 64];
+  __shared__ double z[WALK ? 1 : kMaxTree], tmp[kThreads / 64];
   const int chunk = blockIdx.x % a.n_chunks, r = blockIdx.x / a.n_chunks;
-  Last last(a, r);
-  if (last.node < 0) return;
-  last.read(a, chunk, false, gone, &n_gone, z);
-  const double s = group_sum(last.sum(), tmp);
-  if (threadIdx.x == 0) a.sums[(int64_t)r * a.n_chunks + chunk] = s;
+  auto sum = [&](Last last) {
+    if (last.node < 0) return;
+    last.read(a, chunk, false, gone, &n_gone, z);
+    const double s = group_sum(last.sum(), tmp);
+    if (threadIdx.x == 0) a.sums[(int64_t)r * a.n_chunks + chunk] = s;
+  };
+  if constexpr (WALK) {
+    __shared__ WalkShared sh;
+    const Walk w = walk(a, r, chunk == 0, sh);
+    sum(Last(a, w, sh));
+  } else {
+    sum(Last(a, r));
+  }
 }
 
 // The sums of the threads' values before this one's, and of all
@@ -339,10 +373,15 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
 int verify_chunks(int V) { return (V + kPart - 1) / kPart; }
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
-  verify_walk_kernel<<<a.R, kThreads, 0, s>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  verify_sums_kernel<<<(unsigned)((int64_t)a.R * a.n_chunks), kThreads, 0, s>>>(a);
+  const unsigned groups = (unsigned)((int64_t)a.R * a.n_chunks);
+  hipError_t e;
+  if (a.draft) {
+    verify_walk_kernel<<<a.R, kThreads, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    verify_sums_kernel<false><<<groups, kThreads, 0, s>>>(a);
+  } else {
+    verify_sums_kernel<true><<<groups, kThreads, 0, s>>>(a);
+  }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   verify_pick_kernel<<<a.R, kThreads, 0, s>>>(a);
   return hipGetLastError();
