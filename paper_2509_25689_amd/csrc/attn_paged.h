@@ -552,12 +552,16 @@ struct Work {
   // The units are cut into runs: kRuns equal ones (a power of two), or one unit
   // each where there are fewer.
   static constexpr int kRuns = FEW ? kFewGroups : kTileGroups;
+  // Trees are tiles of few rows over many keys, whose pieces' sums are as large as the
+  // keys: where runs would be short, half as many (one request's 24 tokens over 8192
+  // keys @@).
+  static __device__ __forceinline__ int runs(int n) { return TREE && !FEW && n < 8 * kRuns ? kRuns / 2 : kRuns; }
   static __device__ __forceinline__ int run_start(int n, int w) {
-    return n < kRuns ? min(w, n) : (int)((uint64_t)(uint32_t)n * (uint32_t)w / kRuns);
+    return n < runs(n) ? min(w, n) : (int)((uint64_t)(uint32_t)n * (uint32_t)min(w, runs(n)) / runs(n));
   }
   // runs that start before unit u (0 < u <= n)
   static __device__ __forceinline__ int runs_before(int n, int u) {
-    return n < kRuns ? u : (int)(((uint64_t)(uint32_t)u * kRuns + n - 1) / (uint32_t)n);
+    return n < runs(n) ? u : (int)(((uint64_t)(uint32_t)u * runs(n) + n - 1) / (uint32_t)n);
   }
   // requests of at most few_rows (32, or less) go to the few-rows kernel, the others to tiles
   static __device__ __forceinline__ int row_tiles(const AttnArgs& a, const Seq& s) {
@@ -647,7 +651,7 @@ __device__ __forceinline__ void each_piece(const AttnArgs& a, int* tmp, PagedJoi
     N = total * a.HK;
     // Workgroup b runs on XCD b % 8: an XCD's runs are neighbours, whose row
     // tiles share keys and values
-    if (!W::kFew && N >= W::kRuns) w = (w & 7) * (W::kRuns / 8) + (w >> 3);
+    if (!W::kFew && N >= W::runs(N) && w < W::runs(N)) w = (w & 7) * (W::runs(N) / 8) + (w >> 3);
     // Single rows share nothing, but the heads of a page lie side by side: they
     // are read at the same time, by neighbouring workgroups
     if (W::kFew && N >= W::kRuns && W::kRuns % a.HK == 0) w = w % a.HK * (W::kRuns / a.HK) + w / a.HK;

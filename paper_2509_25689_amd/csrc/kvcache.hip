@@ -269,6 +269,13 @@ __global__ __launch_bounds__(256) void commit_kernel(CommitArgs a, int groups) {
   const int r = blockIdx.x / groups, i = (blockIdx.x - r * groups) * 256 + threadIdx.x;
   const bool val = blockIdx.y;
   const int C = val ? a.vchunks : a.kchunks, chunks = a.HK * C;
+  const int32_t* path = a.path + (int64_t)r * a.path_stride;
+  // (the first numbers of the path before it is known how many count: a read less in
+  // the chain)
+  const int64_t ctx = a.ctx[r];
+  int p[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) p[u] = path[min(u, a.width - 1)];
   const int n = min(a.counts[r], a.width);
   if (n < 2 || i >= chunks + (a.ks ? a.HK : 0)) return;
   const bool scale = i >= chunks;
@@ -284,8 +291,7 @@ __global__ __launch_bounds__(256) void commit_kernel(CommitArgs a, int groups) {
     page_bytes = val ? a.v_page : a.k_page;
     row_bytes = val ? a.v_row : a.k_row;
   }
-  const int64_t ctx = a.ctx[r];
-  const int32_t *path = a.path + (int64_t)r * a.path_stride, *table = a.table + (int64_t)r * a.table_stride;
+  const int32_t* table = a.table + (int64_t)r * a.table_stride;
   auto at = [&](int64_t pos) -> char* {
     const int64_t b = pos >> a.page_shift;
     if (pos < 0 || b >= a.max_blocks) return nullptr;
@@ -294,12 +300,15 @@ __global__ __launch_bounds__(256) void commit_kernel(CommitArgs a, int groups) {
     return base + page * page_bytes + (pos & ((1 << a.page_shift) - 1)) * row_bytes;
   };
   for (int j0 = 0; j0 < n; j0 += U) {
+    if (j0)
+#pragma unroll
+      for (int u = 0; u < U; ++u) p[u] = path[min(j0 + u, a.width - 1)];
     char *from[U], *to[U];
     u32x4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int j = j0 + u, p = j < n ? path[j] : j;
-      from[u] = p > j ? at(ctx + p) : nullptr;  // (p == j: there already)
+      const int j = j0 + u;
+      from[u] = j < n && p[u] > j ? at(ctx + p[u]) : nullptr;  // (j itself: there already)
       to[u] = from[u] ? at(ctx + j) : nullptr;
     }
 #pragma unroll
