@@ -553,9 +553,10 @@ struct Work {
   // each where there are fewer.
   static constexpr int kRuns = FEW ? kFewGroups : kTileGroups;
   // Trees are tiles of few rows over many keys, whose pieces' sums are as large as the
-  // keys: where runs would be short, half as many (one request's 24 tokens over 8192
-  // keys @@).
-  static __device__ __forceinline__ int runs(int n) { return TREE && !FEW && n < 8 * kRuns ? kRuns / 2 : kRuns; }
+  // keys: where runs would be shorter than 5 units, half as many (one request's 24 tokens
+  // over 8192 keys: tiles and join 33 us, 37 with all; over 16000 keys 44 either way, and
+  // 48 requests' trees over about 400 keys 55, 47 with all).
+  static __device__ __forceinline__ int runs(int n) { return TREE && !FEW && n < 5 * kRuns ? kRuns / 2 : kRuns; }
   static __device__ __forceinline__ int run_start(int n, int w) {
     return n < runs(n) ? min(w, n) : (int)((uint64_t)(uint32_t)n * (uint32_t)min(w, runs(n)) / runs(n));
   }
@@ -953,9 +954,9 @@ __device__ __forceinline__ int join_run() {
 // Adds up the pieces of cut segments: of tiled rows, workgroup (w, b) the b-th 32
 // columns of a segment, each wave its 32 rows, in the registers' order.  Bound by the
 // reads' latency where few segments are cut into many pieces, so U of them are in
-// flight (one request's tree of 24 tokens over 8192 keys, 16 segments of 32 pieces:
-// 70 us with all columns in one workgroup and a piece at a time, @@); by memory with
-// many (up to 134 MB of sums).
+// flight (16 segments of 32 pieces, one request's tree of 24 tokens: 14 to 20 us, with
+// all columns in one workgroup and a piece at a time 70); by memory with many (up to
+// 134 MB of sums: chunks of four prompts 15 us).
 template <typename T, int DV, int NW>
 __global__ __launch_bounds__(64 * NW) void tile_join_kernel(AttnArgs a) {
   constexpr int U = 4;
