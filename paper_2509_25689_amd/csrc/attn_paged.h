@@ -902,7 +902,6 @@ __global__ __launch_bounds__(64 * NW, 1) void paged_few_kernel(AttnArgs a) {
     const Row row = row_of(a, s, lane & 31);
     rb.load_q(q_row(a, s, row, kvh));
     rb.clear();
-    rb.wait_q();
     See see{};
     if constexpr (TREE) see.set(a, s, row.valid ? row.token : -1, lds_addr(parents));
     const int top = min(row.see.hi, s.kv);
