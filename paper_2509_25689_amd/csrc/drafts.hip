@@ -30,6 +30,7 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 // the workgroup's sum, for every thread; tmp: a double for each wave
+template <int NT>
 __device__ __forceinline__ double group_sum(double v, double* tmp) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   v = wave_sum(v);
@@ -38,7 +39,7 @@ __device__ __forceinline__ double group_sum(double v, double* tmp) {
   __syncthreads();
   double all = 0.0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) all += tmp[w];
+  for (int w = 0; w < NT / 64; ++w) all += tmp[w];
   return all;
 }
 
@@ -69,24 +70,26 @@ __device__ __forceinline__ double residual(float p, float q, const double* z, in
 
 // The walk of request r by one workgroup, every wave on the same way; where a sibling
 // after a rejected one is tried, the whole workgroup sums the residual.
+template <int NT>
 struct WalkShared {
   int parent[kMaxTree], token[kMaxTree];
   float px[kMaxTree], qx[kMaxTree], u[kMaxTree];
-  double z[kMaxTree], tmp[kThreads / 64];
+  double z[kMaxTree], tmp[NT / 64];
   int n_gone;
 };
 struct Walk {
   int first, n, node, count, rejected;  // node -1: nothing to keep, or left out
 };
 // write: the path and what follows from it (one workgroup of a request's)
-__device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, WalkShared& sh) {
+template <int NT>
+__device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, WalkShared<NT>& sh) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int first = min(max(a.cu[r], 0), a.T), n = min(max(a.cu[r + 1], first), a.T) - first;
   int32_t *path = a.path + (int64_t)r * a.width, *out = a.out + (int64_t)r * a.width;
   VerifyEnd* end = a.end + r;
   if (n < 1 || n > kMaxTree || n > a.width) {
     if (write) {
-      for (int i = tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
+      for (int i = tid; i < a.width; i += NT) path[i] = out[i] = -1;
       if (tid == 0) {
         a.counts[r] = 0;
         end->node = -1;
@@ -94,7 +97,7 @@ __device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, Wal
     }
     return Walk{first, 0, -1, 0, 0};
   }
-  static_assert(kThreads == kMaxTree, "a thread a token");
+  static_assert(NT >= kMaxTree, "a thread a token");
   if (tid == 0) sh.n_gone = 0;
   if (tid < n) {
     const int p = a.parents[first + tid], x = a.tokens[first + tid];
@@ -125,14 +128,14 @@ __device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, Wal
             // (siblings after a rejected one alone take a pass over the row)
             const float *p = a.target + (int64_t)(first + at) * a.target_row, *q = a.draft + (int64_t)(first + at) * a.draft_row;
             double sum = 0.0;
-            for (int j = tid * kPer; j < a.V; j += kPart) {
+            for (int j = tid * kPer; j < a.V; j += NT * kPer) {
               float pv[kPer], qv[kPer];
               read_row(p, j, a.V, pv);
               read_row(q, j, a.V, qv);
 #pragma unroll
               for (int i = 0; i < kPer; ++i) sum += residual(pv[i], qv[i], sh.z, rejected);
             }
-            total = group_sum(sum, sh.tmp);
+            total = group_sum<NT>(sum, sh.tmp);
             rx = residual(sh.px[c], sh.qx[c], sh.z, rejected);
           }
         } else if (there && rejected > 0) {
@@ -164,7 +167,7 @@ __device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, Wal
     }
   }
   if (write) {
-    for (int i = count + tid; i < a.width; i += kThreads) path[i] = out[i] = -1;
+    for (int i = count + tid; i < a.width; i += NT) path[i] = out[i] = -1;
     if (tid == 0) {
       a.counts[r] = count;
       end->node = at;
@@ -181,9 +184,12 @@ __device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, Wal
   return Walk{first, n, at, count, rejected};
 }
 
-// One workgroup a request
-__global__ __launch_bounds__(kThreads) void verify_walk_kernel(VerifyArgs a) {
-  __shared__ WalkShared sh;
+// One workgroup a request, of as many threads as there are: a pass over two rows of
+// 128000 (1 MB) takes 15 us, with 256 threads 35 (reads of a step ahead do not gain: a
+// third of it is float64 arithmetic); 48 chains, which need none, 8 us instead of 6.
+constexpr int kWalkThreads = 1024;
+__global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyArgs a) {
+  __shared__ WalkShared<kWalkThreads> sh;
   walk(a, blockIdx.x, true, sh);
 }
 
@@ -194,7 +200,7 @@ struct Last {
   double r[kPer];
   double z;   // with draft rows: the sum before rejection tid
   int token;  // without: what rejection tid took
-  __device__ __forceinline__ Last(const VerifyArgs& a, const Walk& w, const WalkShared& sh)
+  __device__ __forceinline__ Last(const VerifyArgs& a, const Walk& w, const WalkShared<kThreads>& sh)
       : node(w.node), rejected(w.rejected), first(w.first), z(0.0) {  // (without draft rows)
     token = (int)threadIdx.x < w.n && sh.parent[threadIdx.x] == w.node ? sh.token[threadIdx.x] : -1;
   }
@@ -258,11 +264,11 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyArgs a) {
   auto sum = [&](Last last) {
     if (last.node < 0) return;
     last.read(a, chunk, false, gone, &n_gone, z);
-    const double s = group_sum(last.sum(), tmp);
+    const double s = group_sum<kThreads>(last.sum(), tmp);
     if (threadIdx.x == 0) a.sums[(int64_t)r * a.n_chunks + chunk] = s;
   };
   if constexpr (WALK) {
-    __shared__ WalkShared sh;
+    __shared__ WalkShared<kThreads> sh;
     const Walk w = walk(a, r, chunk == 0, sh);
     sum(Last(a, w, sh));
   } else {
@@ -335,7 +341,7 @@ __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
     if (whole)
       for (int c = 0; c < a.n_chunks; ++c) {
         row.read(a, c, true, gone, &n_gone, z);
-        const double s = group_sum(row.sum(), tmp);
+        const double s = group_sum<kThreads>(row.sum(), tmp);
         if (tid == c) chunk_sum = s;
       }
     const Scan in = group_scan(chunk_sum, tmp);  // (of chunk tid)
@@ -376,7 +382,7 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
   const unsigned groups = (unsigned)((int64_t)a.R * a.n_chunks);
   hipError_t e;
   if (a.draft) {
-    verify_walk_kernel<<<a.R, kThreads, 0, s>>>(a);
+    verify_walk_kernel<<<a.R, kWalkThreads, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     verify_sums_kernel<false><<<groups, kThreads, 0, s>>>(a);
   } else {
