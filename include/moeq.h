@@ -677,7 +677,9 @@ moeq_status moeq_verify_workspace(int32_t n_requests, int32_t vocab, uint64_t* b
  *   path     DEVICE int32 [n_requests x max_path], rows path_stride apart: ascending from
  *            0 on (moeq_verify's; of a row that is not, what is moved is unspecified, but
  *            lies within the cache)
- *   counts, ctx_lens  DEVICE int32 [n_requests]
+ *   counts, ctx_lens  DEVICE int32 [n_requests]; counts beyond max_path count as it.  A
+ *            request that the step's plan refused has a count of 0 or 1: its table's entries
+ *            behind the context may be pages of others
  *   block_table  as for moeq_attn_paged; positions in no page of the cache are left out
  * No two requests' tables may share the pages behind their contexts.
  * Errors: INVALID_ARG, UNSUPPORTED, DEVICE. */

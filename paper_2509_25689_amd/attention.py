@@ -107,7 +107,8 @@ def append(k_cache, v_cache, k, v, slots, *, scales=None, stream=None):
 def commit(k_cache, v_cache, path, counts, ctx_lens, block_table, *, scales=None, stream=None):
     """Keeps the drafted tokens path[r, :counts[r]] (int32 [R, any], numbers among the
     request's new tokens, ascending from 0) in the cache: their keys and values move to
-    the places right behind the ctx_lens[r] tokens before them."""
+    the places right behind the ctx_lens[r] tokens before them.  A request that the
+    step's plan refused (kv_lens[r] is 0) needs a count of 0."""
     _c.commit(k_cache, v_cache, path, counts, ctx_lens, block_table, scales, stream)
 
 

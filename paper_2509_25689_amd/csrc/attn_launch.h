@@ -29,8 +29,9 @@ hipError_t launch_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws
     a.whole = a.max_kv <= 512;
     // Which requests the few-rows kernel takes: those of up to 32 rows.  Over codes those
     // of up to 16 where no other is there, or where the others go to tiles: 48 requests
-    // of 7 rows take 62 us a call so and 65 in blocks of 32.  A step of trees larger than that is left to the tiles whole: a small
-    // tree among them costs less there than two more launches.
+    // of 7 rows take 62 us a call so and 65 in blocks of 32.  A step of trees larger than
+    // that is left to the tiles whole: a small tree among them costs less there than two
+    // more launches.
     a.few_rows = TREE && tiles ? 0 : E4M3 && a.g <= 16 && (tiles || max_rows <= 16) ? 16 : kFewRows;
     hipError_t e = hipSuccess;
     if (a.few_rows == 0) {

@@ -66,8 +66,9 @@ __device__ __forceinline__ void decode16(u32x4 x, float scale, u32x4& lo, u32x4&
 // 2^(byte - 127)
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// Where a request's keys and values lie in an e4m3 cache: a granule of 16 goes through the registers, where its codes
-// become values of T, and lies in LDS as that of a 16-bit cache does.
+// Where a request's keys and values lie in an e4m3 cache.  For tiles a granule of 16
+// goes through the registers, where its codes become values of T, and lies in LDS as
+// that of a 16-bit cache does.
 template <typename T, int D, int DV>
 struct Keys8 {
   const AttnArgs& a;
@@ -354,7 +355,11 @@ struct TileKernel {
   // Codes go through the registers: a tile's are read while the one before it is taken,
   // decoded between the steps of its scores and written as values to the other stage.
   // The loads stay in flight across the barrier, which waits for LDS alone.  (The scores
-  // of a tile ahead, as below, do not fit the registers beside the codes.)
+  // of a tile ahead, as below, do not fit the registers beside the codes; nor do the
+  // codes of two tiles with 128-wide heads, and 64-wide ones lose: 48 trees 103 us
+  // against 114.)  48 trees of up to 24 tokens over 400 MB of codes 156 us, 16-bit values
+  // of the same 152: matrix units busy 31 %, vector units 39 %, waits 45 %.  Waves without
+  // rows take every step as the others do: told to load alone, they gain nothing (159).
   template <typename F>
   static __device__ __forceinline__ void run_codes(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
                                                    const K& keys, const Row& r, const See& see, int lo, int hi, Span all,
@@ -832,9 +837,9 @@ __device__ __forceinline__ void few_finish(const AttnArgs& a, F store, float m_o
 // each of a tile of 32 NW, through two LDS stages of their own, and join their
 // sums at the end of a piece.  Bound by memory: a compute unit has 128 KB of loads in
 // flight with 128-wide heads, 120 with 192-wide ones, 64 with 64-wide ones (48
-// requests over 311 MB of those 67 us a call, 4.7 TB/s).  128 requests over 3.94 GB of cache 606 us (6.5 TB/s; a streaming read
-// reaches 6.95), 48 over 727 MB 115 us, one over 134 MB 26 us (ramp and the uneven
-// end of 8 or 9 tiles a workgroup).  Runs cut at 32 keys instead of 128 are more
+// requests over 311 MB of those 67 us a call, 4.7 TB/s).  128 requests over 3.94 GB of
+// cache 606 us (6.5 TB/s; a streaming read reaches 6.95), 48 over 727 MB 115 us, one over
+// 134 MB 26 us (ramp and the uneven end of 8 or 9 tiles a workgroup).  Runs cut at 32 keys instead of 128 are more
 // even but slower (48 requests' calls 122 to 128 us, 100 over 1500 keys 67 to 74):
 // the waves of a workgroup then end at different times.
 template <typename T, int D, int DV, int NW>

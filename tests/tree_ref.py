@@ -40,10 +40,8 @@ def causal_mask(n, kv, window=0):
     return seen & (s[None] > p[:, None] - window) if window else seen
 
 
-def attend(q, k, v, seen, scale, dtype, small=0.0):
-    """q [L, HQ, D], k [S, HK, D], v [S, HK, DV], seen [L, S] -> (o [L, HQ, DV], bound, lse [L, HQ], lse bound).
-    small: what a weight loses below the products' normal range, relative to its row's
-    largest product of weight and value (beside attn_ref's z)."""
+def attend(q, k, v, seen, scale, dtype):
+    """q [L, HQ, D], k [S, HK, D], v [S, HK, DV], seen [L, S] -> (o [L, HQ, DV], bound, lse [L, HQ], lse bound)."""
     L, HQ, D = q.shape
     S, HK = k.shape[:2]
     g = HQ // HK
@@ -73,8 +71,6 @@ def attend(q, k, v, seen, scale, dtype, small=0.0):
         dx = (D + 4) * 2.0 ** -24 * size
         d = 2 * dx + 3 * 2.0 ** -23 * big + (n + 16) * 2.0 ** -23
         z = 2.0 ** -25 * (seen.double() @ va.abs() + 1) if dtype == torch.float16 else 0.0
-        if small:
-            z = z + small * n * va.abs().amax()
         o[some, h] = oh
         tol[some, h] = 1.05 * ((u + d) * (w @ va.abs()) + u * oh.abs() + z)
         lse[some, h] = torch.logsumexp(x, 1)
