@@ -75,8 +75,9 @@ __device__ __forceinline__ u32x4 values8(u32x2 c) {
 }
 
 // One wave's state for 32 query rows, on RowBlock's.  A tile's keys lie at kt, its
-// values at vt and its scales at sc in LDS.
-template <typename T, int D, int DV>
+// values at vt and its scales at sc in LDS: 16 keys' and their values', and those of the
+// other 16 keys GAP bytes further.
+template <typename T, int D, int DV, int GAP = 32>
 struct Codes32 : RowBlock<T, D, DV, true> {
   static constexpr int ROWS = 32, kTerms = std::is_same_v<T, F16> ? 2 : 1, CK = D / 16, CV = DV / 16;
   static constexpr bool kPairs = true;
@@ -104,9 +105,9 @@ struct Codes32 : RowBlock<T, D, DV, true> {
   }
   __device__ __forceinline__ Scales read_scales(uint32_t sc) const {
     const int lane = threadIdx.x & 63;
-    Scales s{scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + (lane & 31))), {}};
+    Scales s{scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + GAP * (lane >> 4 & 1) + (lane & 15))), {}};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s.v[j] = lds_read4(sc + 32 + 8 * j + 4 * (lane >> 5));
+    for (int j = 0; j < 4; ++j) s.v[j] = lds_read4(sc + GAP * (j >> 1) + 16 + 8 * (j & 1) + 4 * (lane >> 5));
     return s;
   }
   __device__ __forceinline__ Keys read_keys(uint32_t kt) const {
@@ -137,6 +138,10 @@ struct Codes32 : RowBlock<T, D, DV, true> {
   static __device__ __forceinline__ void mask(X& x, int first, int lo, int hi) { RB::mask(x[0], first, lo, hi); }
   static __device__ __forceinline__ void mask_bits(X& x, uint32_t bits) { RB::mask_bits(x[0], bits); }
   __device__ __forceinline__ void rescale(const X& x, float c) { RB::rescale(RB::template largest<1>(x), c); }
+  __device__ __forceinline__ void rescale(const X& x, const X& y, float c) {
+    const f32x16 both[2] = {x[0], y[0]};
+    RB::rescale(RB::template largest<2>(both), c);
+  }
   __device__ __forceinline__ void values(const X& x, float c, const Scales& sc, const Values& v) {
     uint32_t p[8][kTerms];
 #pragma unroll
@@ -213,8 +218,8 @@ struct Codes16 {
     Scales s;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      s.k[b] = scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + 16 * b + (lane & 15)));
-      s.v[b] = lds_read4(sc + 32 + 16 * b + 4 * (lane >> 4));
+      s.k[b] = scale_of(*(const MOEQ_LDS uint8_t*)(uintptr_t)(sc + 32 * b + (lane & 15)));
+      s.v[b] = lds_read4(sc + 32 * b + 16 + 4 * (lane >> 4));
     }
     return s;
   }
@@ -354,8 +359,8 @@ struct Codes16 {
 };
 
 // ---- the kernel ----
-// A stage holds 32 keys, their values and, in its last 256 bytes, both scales (32 bytes
-// each; the load fills the rest with the same).  128 KB of LDS or more are in flight:
+// A stage holds 32 keys, their values and, in its last 256 bytes, both scales (64 bytes;
+// the load fills the rest with the same).  128 KB of LDS or more are in flight:
 // eight waves of two stages with 128-wide heads.
 constexpr int few8_waves(int D) { return D == 192 ? 6 : 8; }
 template <int D, int DV, int ROWS>
@@ -431,14 +436,14 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
         o.load(p, dst);
       }
     };
-    // a lane's dword of the scales: 16 bytes of each granule's keys, then of its values
-    const char* scales = (const char*)(lane & 8 ? keys.vs : keys.ks) + 4 * (lane & 3);
-    const int64_t scale_page = lane & 8 ? a.vs_page : a.ks_page;
+    // a lane's dword of the scales: 16 bytes of a granule's keys, then of its values
+    const char* scales = (const char*)(lane & 4 ? keys.vs : keys.ks) + 4 * (lane & 3);
+    const int64_t scale_page = lane & 4 ? a.vs_page : a.ks_page;
     auto load_k = [&](uint32_t st, const Two& t, auto full) {
       const int page0 = keys.valid(t.page0), page1 = keys.valid(t.page1);
       granule_k(t.g0, page0, st, full);
       granule_k(t.g1, page1, st + kGranule * D, full);
-      load_lds4(scales + (lane & 4 ? page1 : page0) * scale_page + (lane & 4 ? keys.place(t.g1) : keys.place(t.g0)),
+      load_lds4(scales + (lane & 8 ? page1 : page0) * scale_page + (lane & 8 ? keys.place(t.g1) : keys.place(t.g0)),
                 st + FK::kK + FK::kV);
     };
     auto load_v = [&](uint32_t st, const Two& t, auto full) {
@@ -522,6 +527,168 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
     few_finish<T, DV, NW, ROWS>(a, [&](float* p, float f) { rb.store(p, f); }, rb.m, rb.sum(), smem, FK::kWave, ml, s, kvh,
                                 whole, slot);
     __syncthreads();
+  });
+}
+
+// Requests of more rows, of trees: tiles of 64 keys, which the workgroup's waves share
+// and keep 32 rows each, as TileKernel, but of codes, several of them in flight.  Every
+// wave decodes every key and value (370 vector instructions a tile for 290 where one
+// does), and the registers that the codes no longer pass hold the next tile's scores.
+// 48 trees of up to 16 tokens of 7 heads over 400 MB of codes: 150 us, TileKernel 159;
+// with heads of 192 131 against 195 (the scores a tile ahead again), of 64 102 either
+// way.  Chunks of 512 tokens, whose rows are many, 358 either way, with heads of 64 135
+// against 124; in binary16, where values take two terms, trees 153 against 139 and
+// chunks 384 against 312.  Matrix units busy 29 %, vector units 53 %, waits 25 %.
+template <typename T, int D, int DV>
+struct TileKernel8 {
+  static constexpr int NW = 4, BM = 32 * NW;
+  static constexpr int S = D == 192 ? 3 : 4;  // stages; two workgroups a compute unit
+  static constexpr uint32_t kK = kTileKeys * D, kV = kTileKeys * DV, kStage = kK + kV + 256 * NW;
+  static constexpr int kLoads = D / 64 + DV / 64 + 1;  // of a stage, a wave's
+  static constexpr uint32_t kScratch = (S - 1) * kStage;  // (a stage that is loaded behind the first barrier)
+  static constexpr size_t lds = S * kStage;
+  static_assert(NW * kGranule == kTileKeys, "a wave loads one granule of a tile");
+};
+
+template <typename T, int D, int DV>
+__global__ __launch_bounds__(256, 2) void paged_tile8_kernel(AttnArgs a) {
+  typedef TileKernel8<T, D, DV> TK;
+  typedef Work<TK::BM, kTileKeys, false, true> W;
+  typedef Codes32<T, D, DV, 256> Block;
+  constexpr int NW = TK::NW, S = TK::S, CK = D / 16, CV = DV / 16;
+  extern __shared__ __align__(128) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t base = lds_addr(smem);
+  Block rb;
+  rb.set();
+  Keys8<T, D, DV> keys(a);
+  GranuleOffsets8<CK, false> ko;
+  GranuleOffsets8<CV, Block::kPairs> vo;
+  ko.set(a.k_row, kGranule - 1);
+  vo.set(a.v_row, kGranule - 1);
+  each_piece<W, 64 * NW>(a, (int*)(smem + TK::kScratch), a.tile_join, [&](int kvh, int r, const Seq& s, int qt, const Span& sp, int t0, int n, bool whole, int slot) {
+    keys.seq(s, r, kvh);
+    const int lo = sp.lo + t0 * kTileKeys, hi = min(sp.hi, lo + n * kTileKeys);
+    const Order od(lo, hi, kTileKeys, kTileKeys, Span{0, max(s.kv - s.n, 0)});
+    auto granule = [&](int key) { return keys.granule(key + wave * kGranule); };
+    const char* scales = (const char*)(lane & 4 ? keys.vs : keys.ks) + 4 * (lane & 3);
+    const int64_t scale_page = lane & 4 ? a.vs_page : a.ks_page;
+    // this wave's granule g of a tile, whose page the table's `entry` is, into stage st
+    auto load = [&](int g, int entry, uint32_t st) {
+      const int page = keys.valid(entry), place = keys.place(g);
+      const char *k = keys.k + page * a.k_page + (uint64_t)(uint32_t)place * a.k_row,
+                 *v = keys.v + page * a.v_page + (uint64_t)(uint32_t)place * a.v_row;
+      const uint32_t kd = st + wave * (kGranule * D), vd = st + TK::kK + wave * (kGranule * DV);
+      if (g + kGranule <= s.kv) {
+        ko.load(k, kd);
+        vo.load(v, vd);
+      } else {  // (rows past the last key repeat it)
+        GranuleOffsets8<CK, false> kt;
+        GranuleOffsets8<CV, Block::kPairs> vt;
+        kt.set(a.k_row, s.kv - 1 - g);
+        vt.set(a.v_row, s.kv - 1 - g);
+        kt.load(k, kd);
+        vt.load(v, vd);
+      }
+      load_lds4(scales + page * scale_page + place, st + TK::kK + TK::kV + 256 * wave);
+    };
+    int g_next = 0, entry = 0;  // of tile i + S - 1, looked up while tile i - 1 is taken
+    if (od.n > 0) {
+      int g[S], e[S];
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        g[i] = granule(od.key(min(i, od.n - 1)));
+        e[i] = keys.entry(g[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < S - 1; ++i)
+        if (i < od.n) load(g[i], e[i], base + i * TK::kStage);
+      g_next = g[S - 1];
+      entry = e[S - 1];
+    }
+    const Row row = row_of(a, s, qt * TK::BM + wave * 32 + (lane & 31));
+    rb.load_q(q_row(a, s, row, kvh));
+    rb.clear();
+    // (the scratch is free until the first barrier, but for find_place's numbers)
+    SeeTree see;
+    see.set(a, s, row.valid ? row.token : -1, base + TK::kScratch + 256);
+    rb.wait_q();
+    const int top = min(row.see.hi, s.kv);
+    uint32_t st = 0;  // of the tile that is taken
+    auto before = [&](uint32_t st) { return st == 0 ? (S - 1) * TK::kStage : st - TK::kStage; };
+    auto after = [&](uint32_t st) { return st == (S - 1) * TK::kStage ? 0 : st + TK::kStage; };
+    // every wave's part of a tile is there, and what was read before this is read; PAST
+    // tiles behind it are on their way, if `more`
+    auto arrive = [&](auto past, bool more) {
+      if (more)
+        wait_loads<past.value * TK::kLoads>();
+      else
+        wait_loads<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    };
+    auto load_next = [&](int i) {  // tile i + S - 1, into the stage before tile i's
+      if (i + S - 1 < od.n) {
+        load(g_next, entry, base + before(st));
+        g_next = granule(od.key(min(i + S, od.n - 1)));
+        entry = keys.entry(g_next);
+      }
+    };
+    typedef typename Block::X X;
+    auto scores = [&](uint32_t st, X& x0, X& x1) {
+      const uint32_t kt = base + st, sc = kt + TK::kK + TK::kV;
+      rb.scores(x0, rb.read_keys(kt), rb.read_scales(sc));
+      rb.scores(x1, rb.read_keys(kt + 32 * D), rb.read_scales(sc + 512));
+    };
+    auto finish = [&](uint32_t st, const X& x0, const X& x1) {
+      const uint32_t vt = base + st + TK::kK, sc = vt + TK::kV;
+      rb.values(x0, a.c, rb.read_scales(sc), rb.read_values(vt));
+      rb.values(x1, a.c, rb.read_scales(sc + 512), rb.read_values(vt + 32 * DV));
+    };
+    int i = 0;
+    for (; i < od.masked; ++i) {
+      arrive(std::integral_constant<int, S - 2>(), i + S - 2 < od.n);
+      load_next(i);
+      X x0, x1;
+      scores(st, x0, x1);
+      const int key = od.key(i);
+      Block::mask(x0, key, row.see.lo, top);
+      Block::mask(x1, key + 32, row.see.lo, top);
+      Block::mask_bits(x0, see.window(key));
+      Block::mask_bits(x1, see.window(key + 32));
+      rb.rescale(x0, x1, a.c);
+      finish(st, x0, x1);
+      st = after(st);
+    }
+    if (od.masked > 0 && !rb.finite())
+      rb.redo(a.c, row.see.lo, top, od.masked, kTileKeys, hi, keys, [&](int i) { return od.key(i); }, see);
+    if (i < od.n) {
+      // the others, one ahead, as TileKernel's
+      auto step = [&](int i, const X& x0, const X& x1, X& y0, X& y1) {
+        rb.rescale(x0, x1, a.c);
+        arrive(std::integral_constant<int, S - 3>(), i + S - 2 < od.n);
+        load_next(i);
+        const uint32_t next = after(st);
+        scores(next, y0, y1);
+        finish(st, x0, x1);
+        st = next;
+      };
+      X x0, x1, y0, y1;
+      arrive(std::integral_constant<int, S - 2>(), i + S - 2 < od.n);
+      scores(st, x0, x1);
+      for (; i + 2 < od.n; i += 2) {
+        step(i, x0, x1, y0, y1);
+        step(i + 1, y0, y1, x0, x1);
+      }
+      if (i + 1 < od.n) {
+        step(i++, x0, x1, y0, y1);
+        x0[0] = y0[0];
+        x1[0] = y1[0];
+      }
+      rb.rescale(x0, x1, a.c);
+      finish(st, x0, x1);
+    }
+    stage_barrier();
+    store_tile<T, DV>(a, rb.o, rb.m, rb.sum(), s, row, kvh, whole, slot * NW + wave);
   });
 }
 

@@ -58,9 +58,16 @@ hipError_t launch_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws
     if (e != hipSuccess) return e;
     if (tiles) {
       constexpr int NW = kPromptWaves;
-      typedef TileKernel<T, d.value, DV, NW, true, E4M3, TREE> TK;
+      // (what both take: at TileKernel8)
+      constexpr bool kCodes = E4M3 && TREE && std::is_same_v<T, Bf16> && d.value != 64;
+      typedef std::conditional_t<kCodes, TileKernel8<T, d.value, DV>, TileKernel<T, d.value, DV, NW, true, E4M3, TREE>> TK;
       static std::atomic<uint64_t> done{0};
-      auto kernel = paged_tile_kernel<T, d.value, DV, NW, E4M3, TREE>;
+      auto kernel = [&] {
+        if constexpr (kCodes)
+          return paged_tile8_kernel<T, d.value, DV>;
+        else
+          return paged_tile_kernel<T, d.value, DV, NW, E4M3, TREE>;
+      }();
       if ((e = raise_lds_limit((const void*)kernel, done, TK::lds)) != hipSuccess) return e;
       kernel<<<kTileGroups, 64 * NW, TK::lds, s>>>(a);
       if ((e = hipGetLastError()) != hipSuccess) return e;

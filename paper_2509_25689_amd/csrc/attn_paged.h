@@ -722,6 +722,22 @@ __device__ __forceinline__ f32x2v* tile_ml(const AttnArgs& a, int at) {
   return (f32x2v*)a.tile_ml + (int64_t)at * 32 + (threadIdx.x & 31);
 }
 
+// A wave's rows of a piece: whole, or its part
+template <typename T, int DV>
+__device__ __forceinline__ void store_tile(const AttnArgs& a, const f32x16 (&o)[DV / 32], float m, float l, const Seq& s,
+                                           const Row& row, int kvh, bool whole, int at) {
+  if (whole) {
+    store_out<T>(a, o, m, l, s, row, kvh);
+  } else {
+    f32x4* part = tile_part<DV>(a, at);
+#pragma unroll
+    for (int i = 0; i < DV / 8; ++i)
+      part[i * 64] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2],
+                           o[i / 4][4 * (i % 4) + 3]};
+    if ((threadIdx.x & 63) < 32) *tile_ml(a, at) = f32x2v{m, l};
+  }
+}
+
 // Requests of more than 32 rows: the prompt kernel's loop over pages.  Bound as
 // that one is, and by the pieces' sums (written and read once more).  Chunks of
 // four prompts (about 450 tokens of 56 heads each over up to 8700 keys): 320 us.
@@ -752,17 +768,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
       // (stage 1 is free until the first barrier, but for find_place's numbers)
       if constexpr (TREE) see.set(a, s, row.valid ? row.token : -1, lds_addr(smem) + TK::kStage + 256);
     });
-    const float l = sum_halves(rb.l);
-    if (whole) {
-      store_out<T>(a, rb.o, rb.m, l, s, row, kvh);
-    } else {
-      f32x4* part = tile_part<DV>(a, slot * NW + wave);
-#pragma unroll
-      for (int i = 0; i < DV / 8; ++i)
-        part[i * 64] = f32x4{rb.o[i / 4][4 * (i % 4)], rb.o[i / 4][4 * (i % 4) + 1], rb.o[i / 4][4 * (i % 4) + 2],
-                             rb.o[i / 4][4 * (i % 4) + 3]};
-      if (lane < 32) *tile_ml(a, slot * NW + wave) = f32x2v{rb.m, l};
-    }
+    store_tile<T, DV>(a, rb.o, rb.m, sum_halves(rb.l), s, row, kvh, whole, slot * NW + wave);
   });
 }
 
