@@ -357,9 +357,9 @@ struct TileKernel {
   // The loads stay in flight across the barrier, which waits for LDS alone.  (The scores
   // of a tile ahead, as below, do not fit the registers beside the codes; nor do the
   // codes of two tiles with 128-wide heads, and 64-wide ones lose: 48 trees 103 us
-  // against 114.)  48 trees of up to 24 tokens over 400 MB of codes 156 us, 16-bit values
-  // of the same 152: matrix units busy 31 %, vector units 39 %, waits 45 %.  Waves without
-  // rows take every step as the others do: told to load alone, they gain nothing (159).
+  // against 114.)  Chunks of four prompts as below 360 us, in binary16 312: matrix units
+  // busy 34 to 37 %, vector units 41 to 45 %, waits 35 %.  Waves without rows take every
+  // step as the others do: told to load alone, they gain nothing.
   template <typename F>
   static __device__ __forceinline__ void run_codes(const AttnArgs& a, uint32_t base, RB& rb, const typename RB::Addr& ad,
                                                    const K& keys, const Row& r, const See& see, int lo, int hi, Span all,

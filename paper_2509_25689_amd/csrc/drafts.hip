@@ -253,7 +253,7 @@ struct Last {
 };
 
 // The residual's sum over one chunk of the row: workgroup (chunk, request), 16 KB of a
-// row (of two after a rejection): 48 requests over 128000 probabilities (49 MB) 7 us.
+// row (of two after a rejection): 48 requests over 128000 probabilities (49 MB) 10 us.
 // WALK:
 // without draft rows a walk is two reads and a few steps in LDS, and each of a request's
 // workgroups takes it: for one request of 24 tokens 9.3 us a call instead of 12.6
@@ -328,7 +328,7 @@ __device__ __forceinline__ Ends group_ends(int first, int last, int* tmp) {
 }
 
 // The token that follows: one workgroup a request finds the chunk by the sums, then
-// the place in it.  Bound by its chain of two reads and two scans: 7 us.
+// the place in it.  Bound by its chain of two reads and two scans: 6 us.
 __global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyArgs a) {
   __shared__ int gone[kMaxTree], n_gone, ends[2][2 * (kThreads / 64)];
   __shared__ double z[kMaxTree], tmp[kThreads / 64], ahead;
