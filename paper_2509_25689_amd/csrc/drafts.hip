@@ -68,17 +68,18 @@ __device__ __forceinline__ double residual(float p, float q, const double* z, in
   return r;
 }
 
-// The walk of request r by one workgroup, every wave on the same way; where a sibling
-// after a rejected one is tried, the whole workgroup sums the residual.
+// The walk of request r by one workgroup: its first wave goes, and where a sibling after a
+// rejected one is tried, all sum the residual.
+struct Walk {
+  int first, n, node, count, rejected;  // node -1: nothing to keep, or left out
+};
 template <int NT>
 struct WalkShared {
   int parent[kMaxTree], token[kMaxTree];
   float px[kMaxTree], qx[kMaxTree], u[kMaxTree];
   double z[kMaxTree], tmp[NT / 64];
-  int n_gone;
-};
-struct Walk {
-  int first, n, node, count, rejected;  // node -1: nothing to keep, or left out
+  Walk way;
+  int more, n_gone;
 };
 // write: the path and what follows from it (one workgroup of a request's)
 template <int NT>
@@ -109,84 +110,111 @@ __device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, Wal
     sh.qx[tid] = there && a.draft ? a.draft[(int64_t)(first + p) * a.draft_row + x] : 1.0f;
   }
   __syncthreads();
-  int at = 0, count = 1, rejected = 0;
+  Walk w{first, n, 0, 1, 0};
+  double total = 1.0;  // of the residual, if `summed`
+  bool summed = true;
+  // w.node's children not tried yet, of tokens c0 .. c0 + 63
+  uint64_t some = 0;
+  int c0 = 0;
+  auto children = [&](int after) {
+    const int i = c0 + lane;
+    return __ballot(i > after && i < n && sh.parent[min(i, n - 1)] == w.node);
+  };
+  auto next_child = [&]() {  // -1: none
+    while (!some) {
+      c0 += 64;
+      if (c0 >= n) return -1;
+      some = children(0);
+    }
+    const int c = c0 + (int)__builtin_ctzll(some);
+    some &= some - 1;
+    return c;
+  };
+  auto first_child = [&]() {  // (all behind their parent)
+    c0 = w.node & ~63;
+    some = children(w.node);
+    return next_child();
+  };
+  int c = tid < 64 ? first_child() : -1;
   if (write && tid == 0) path[0] = 0;
-  for (int next = 1; next >= 0;) {  // the children of `at`
-    next = -1;
-    rejected = 0;
-    double total = 1.0;
-    for (int c0 = (at + 1) & ~63; c0 < n && next < 0; c0 += 64) {
-      uint64_t some = __ballot(c0 + lane < n && sh.parent[min(c0 + lane, n - 1)] == at);
-      while (some) {
-        const int c = c0 + __builtin_ctzll(some);
-        some &= some - 1;
+  for (;;) {
+    if (tid < 64) {
+      while (c >= 0 && summed) {
         const int x = sh.token[c];
         const bool there = (uint32_t)x < (uint32_t)a.V;
         double rx = sh.px[c];
         if (a.draft) {
-          if (rejected > 0) {
-            // (siblings after a rejected one alone take a pass over the row)
-            const float *p = a.target + (int64_t)(first + at) * a.target_row, *q = a.draft + (int64_t)(first + at) * a.draft_row;
-            double sum = 0.0;
-            for (int j = tid * kPer; j < a.V; j += NT * kPer) {
-              float pv[kPer], qv[kPer];
-              read_row(p, j, a.V, pv);
-              read_row(q, j, a.V, qv);
-#pragma unroll
-              for (int i = 0; i < kPer; ++i) sum += residual(pv[i], qv[i], sh.z, rejected);
-            }
-            total = group_sum<NT>(sum, sh.tmp);
-            rx = residual(sh.px[c], sh.qx[c], sh.z, rejected);
-          }
-        } else if (there && rejected > 0) {
+          rx = residual(sh.px[c], sh.qx[c], sh.z, w.rejected);
+        } else if (there && w.rejected > 0) {
           // what an earlier sibling of the same token took
-          for (int b = at + 1; b < c; ++b)
-            if (sh.parent[b] == at && sh.token[b] == x) rx = 0.0;
+          for (int b = w.node + 1; b < c; ++b)
+            if (sh.parent[b] == w.node && sh.token[b] == x) rx = 0.0;
         }
         if (there && (double)sh.u[c] * (double)sh.qx[c] * total < rx) {
-          next = c;
-          break;
+          if (write && lane == 0) {
+            path[w.count] = c;
+            out[w.count - 1] = x;
+          }
+          ++w.count;
+          w.node = c;
+          w.rejected = 0;
+          total = 1.0;
+          c = first_child();
+          continue;
         }
         if (a.draft) {
-          __syncthreads();
-          if (tid == 0) sh.z[rejected] = total;
-          __syncthreads();
+          if (lane == 0) sh.z[w.rejected] = total;
+          summed = false;
         } else {
           total -= rx;
         }
-        ++rejected;
+        ++w.rejected;
+        c = next_child();
+      }
+      if (lane == 0) {
+        sh.way = w;
+        sh.more = c >= 0;
       }
     }
-    if (next >= 0) {
-      at = next;
-      if (write && tid == 0) {
-        path[count] = at;
-        out[count - 1] = sh.token[at];
-      }
-      ++count;
+    __syncthreads();
+    if (!sh.more) break;
+    // (siblings after a rejected one alone take a pass over the row)
+    const int at = sh.way.node, rejected = sh.way.rejected;
+    const float *p = a.target + (int64_t)(first + at) * a.target_row, *q = a.draft + (int64_t)(first + at) * a.draft_row;
+    double sum = 0.0;
+    for (int j = tid * kPer; j < a.V; j += NT * kPer) {
+      float pv[kPer], qv[kPer];
+      read_row(p, j, a.V, pv);
+      read_row(q, j, a.V, qv);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) sum += residual(pv[i], qv[i], sh.z, rejected);
     }
+    total = group_sum<NT>(sum, sh.tmp);
+    summed = true;
   }
+  w = sh.way;
   if (write) {
-    for (int i = count + tid; i < a.width; i += NT) path[i] = out[i] = -1;
+    for (int i = w.count + tid; i < a.width; i += NT) path[i] = out[i] = -1;
     if (tid == 0) {
-      a.counts[r] = count;
-      end->node = at;
-      end->rejected = rejected;
+      a.counts[r] = w.count;
+      end->node = w.node;
+      end->rejected = w.rejected;
       end->first = first;
     }
     if (a.draft) {
-      if (tid < rejected) end->z[tid] = sh.z[tid];
-    } else if (tid < n && sh.parent[tid] == at) {
+      if (tid < w.rejected) end->z[tid] = sh.z[tid];
+    } else if (tid < n && sh.parent[tid] == w.node) {
       // (all its children are rejected: in any order)
       end->gone[atomicAdd(&sh.n_gone, 1)] = sh.token[tid];
     }
   }
-  return Walk{first, n, at, count, rejected};
+  return w;
 }
 
 // One workgroup a request, of as many threads as there are: a pass over two rows of
 // 128000 (1 MB) takes 15 us, with 256 threads 35 (reads of a step ahead do not gain: a
-// third of it is float64 arithmetic); 48 chains, which need none, 8 us instead of 6.
+// third of it is float64 arithmetic); 48 chains, which need none, 6 us in all (8 with every
+// wave on the way of the first).
 constexpr int kWalkThreads = 1024;
 __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyArgs a) {
   __shared__ WalkShared<kWalkThreads> sh;
