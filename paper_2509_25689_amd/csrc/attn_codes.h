@@ -534,11 +534,16 @@ __global__ __launch_bounds__(64 * few8_waves(D), 1) void paged_few8_kernel(AttnA
 // and keep 32 rows each, as TileKernel, but of codes, several of them in flight.  Every
 // wave decodes every key and value (370 vector instructions a tile for 290 where one
 // does), and the registers that the codes no longer pass hold the next tile's scores.
-// 48 trees of up to 16 tokens of 7 heads over 400 MB of codes: 150 us, TileKernel 159;
-// with heads of 192 131 against 195 (the scores a tile ahead again), of 64 102 either
-// way.  Chunks of 512 tokens, whose rows are many, 358 either way, with heads of 64 135
-// against 124; in binary16, where values take two terms, trees 153 against 139 and
-// chunks 384 against 312.  Matrix units busy 29 %, vector units 53 %, waits 25 %.
+// 48 trees of up to 16 tokens of 7 heads over 400 MB of codes, beside TileKernel (us):
+//   heads of   bfloat16             binary16 (values take two terms)
+//   64         102, 102
+//   128        150, 159             153, 139
+//   192        131, 195             165, 204    (the scores a tile ahead again)
+// with trees of up to 64 tokens 429 and 442 (64: 373, 353), 192 501 and 702, binary16 536
+// and 466, 192 563 and 647.  Chunks of 512 tokens 358 either way, with heads of 64 135
+// and 124, of 192 408 and 428; in binary16 384 and 312, of 192 263 and 224.  So trees of
+// 192-wide heads take it, and of 128-wide ones in bfloat16.  Matrix units busy 29 %,
+// vector units 53 %, waits 25 %.
 template <typename T, int D, int DV>
 struct TileKernel8 {
   static constexpr int NW = 4, BM = 32 * NW;

@@ -59,7 +59,7 @@ hipError_t launch_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws
     if (tiles) {
       constexpr int NW = kPromptWaves;
       // (what both take: at TileKernel8)
-      constexpr bool kCodes = E4M3 && TREE && std::is_same_v<T, Bf16> && d.value != 64;
+      constexpr bool kCodes = E4M3 && TREE && (d.value == 192 || (d.value == 128 && std::is_same_v<T, Bf16>));
       typedef std::conditional_t<kCodes, TileKernel8<T, d.value, DV>, TileKernel<T, d.value, DV, NW, true, E4M3, TREE>> TK;
       static std::atomic<uint64_t> done{0};
       auto kernel = [&] {
