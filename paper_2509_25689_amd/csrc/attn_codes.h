@@ -558,7 +558,7 @@ struct TileKernel8 {
 template <typename T, int D, int DV>
 __global__ __launch_bounds__(256, 2) void paged_tile8_kernel(AttnArgs a) {
   typedef TileKernel8<T, D, DV> TK;
-  typedef Work<TK::BM, kTileKeys, false, true> W;
+  typedef Work<TK::BM, kTileKeys, false, true, true> W;
   typedef Codes32<T, D, DV, 256> Block;
   constexpr int NW = TK::NW, S = TK::S, CK = D / 16, CV = DV / 16;
   extern __shared__ __align__(128) char smem[];

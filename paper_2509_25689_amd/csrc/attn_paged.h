@@ -551,17 +551,24 @@ struct TileKernel {
 // pieces of one leave partial sums that a join kernel adds up.  A workgroup
 // leaves at most two: the piece it starts with (slot 2 w) and the one it ends
 // with (slot 2 w + 1).
-template <int BM, int BN, bool FEW, bool TREE = false>
+template <int BM, int BN, bool FEW, bool TREE = false, bool FEWER = false>
 struct Work {
   static constexpr bool kFew = FEW;
   // The units are cut into runs: kRuns equal ones (a power of two), or one unit
   // each where there are fewer.
   static constexpr int kRuns = FEW ? kFewGroups : kTileGroups;
-  // Trees are tiles of few rows over many keys, whose pieces' sums are as large as the
-  // keys: where runs would be shorter than 5 units, half as many (one request's 24 tokens
-  // over 8192 keys: tiles and join 33 us, 37 with all; over 16000 keys 44 either way, and
-  // 48 requests' trees over about 400 keys 55, 47 with all).
-  static __device__ __forceinline__ int runs(int n) { return TREE && !FEW && n < 5 * kRuns ? kRuns / 2 : kRuns; }
+  // FEWER (trees, and codes): a segment's pieces are read in turn, so where runs would be
+  // shorter than 5 units there are half as many, and then as few as leave 4 units each.
+  // One request's tree of 24 tokens over 8192 keys: tiles and join 33 us, 37 with all;
+  // over 16000 keys 44 either way, and 48 requests' trees over about 400 keys 55, 47 with
+  // all.  A chunk of 8 tokens over 8192 keys 35 us for 45, over 32000 36 for 54; of 6 over
+  // 6200 keys of 2 heads 28 for 40.
+  static __device__ __forceinline__ int runs(int n) {
+    if (!FEWER || n >= 5 * kRuns) return kRuns;
+    int r = kRuns / 2;
+    while (r > 8 && n < 4 * r) r >>= 1;
+    return r;
+  }
   static __device__ __forceinline__ int run_start(int n, int w) {
     return n < runs(n) ? min(w, n) : (int)((uint64_t)(uint32_t)n * (uint32_t)min(w, runs(n)) / runs(n));
   }
@@ -744,7 +751,7 @@ __device__ __forceinline__ void store_tile(const AttnArgs& a, const f32x16 (&o)[
 template <typename T, int D, int DV, int NW, bool E4M3, bool TREE>
 __global__ __launch_bounds__(64 * NW, 2) void paged_tile_kernel(AttnArgs a) {
   typedef TileKernel<T, D, DV, NW, true, E4M3, TREE> TK;
-  typedef Work<TK::BM, kTileKeys, false, TREE> W;
+  typedef Work<TK::BM, kTileKeys, false, TREE, E4M3 || TREE> W;
   extern __shared__ __align__(128) char smem[];  // (16-byte accesses, after any static LDS)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   typename TK::RB rb;
