@@ -558,15 +558,16 @@ struct Work {
   // each where there are fewer.
   static constexpr int kRuns = FEW ? kFewGroups : kTileGroups;
   // FEWER (trees, and codes): a segment's pieces are read in turn, so where runs would be
-  // shorter than 5 units there are half as many, and then as few as leave 4 units each.
-  // One request's tree of 24 tokens over 8192 keys: tiles and join 33 us, 37 with all;
-  // over 16000 keys 44 either way, and 48 requests' trees over about 400 keys 55, 47 with
-  // all.  A chunk of 8 tokens over 8192 keys 35 us for 45, over 32000 36 for 54; of 6 over
-  // 6200 keys of 2 heads 28 for 40.
+  // shorter than 5 units there are half as many, and then as few as leave 3 units each.
+  // Tiles and join, with all runs and so: one request's tree of 24 tokens over 8192 keys 37
+  // and 33 us, over 2000 27 and 24; a chunk of 8 tokens over 8192 keys 45 and 35, of 6 over
+  // 6200 keys of 2 heads 40 and 26 (29 with 4 units).  Longer segments and short ones of
+  // many requests have as many units in all: a tree over 16000 keys takes 44 either way,
+  // 48 over about 400 keys 47 and, with half as many runs, 55.
   static __device__ __forceinline__ int runs(int n) {
     if (!FEWER || n >= 5 * kRuns) return kRuns;
     int r = kRuns / 2;
-    while (r > 8 && n < 4 * r) r >>= 1;
+    while (r > 8 && n < 3 * r) r >>= 1;
     return r;
   }
   static __device__ __forceinline__ int run_start(int n, int w) {
