@@ -139,13 +139,16 @@ def main(shape="tree", cache="bf16", requests=5, n_tokens=40, depth=4, width=3, 
         prompts = _ints([1 if f else 0 for f in fresh]).bool()
         n_new = cu[1:] - cu[:-1]
         path = torch.where(prompts[:, None], torch.arange(path.shape[1], device="cuda").int(), path)
-        counts = torch.where(prompts, n_new, counts)
-        attention.commit(k_cache, v_cache, path, counts, _ints(ctx), table, scales=scales)
+        # (a request that the plan refused keeps nothing and comes again: its kv_lens is 0)
+        counts = torch.where(kv > 0, torch.where(prompts, n_new, counts), 0)
+        attention.commit(k_cache, v_cache, path, counts, _ints(ctx), table, kv_lens=kv, scales=scales)
         pool = attention.trim(kv, _ints(ctx) + counts, table, free, pool, page_size=page_size, pool_out=pool)
         for p, f in enumerate(forest):
             if not f:
                 continue
             r, n = running[p], int(counts[p])
+            if n == 0:
+                continue
             outputs[r].append(y[at[p]: at[p + 1]][path[p, :n].long()])
             ctx[p] += n
             if not fresh[p]:

@@ -678,8 +678,9 @@ moeq_status moeq_verify_workspace(int32_t n_requests, int32_t vocab, uint64_t* b
  *            0 on (moeq_verify's; of a row that is not, what is moved is unspecified, but
  *            lies within the cache)
  *   counts, ctx_lens  DEVICE int32 [n_requests]; counts beyond max_path count as it.  A
- *            request that the step's plan refused has a count of 0 or 1: its table's entries
- *            behind the context may be pages of others
+ *            request that the step's plan refused needs a count of 0 or 1 here (moeq_verify
+ *            counts its tokens as any others'): its table's entries behind the context may
+ *            be pages of others.  moeq_kv_commit_within leaves such a request alone
  *   block_table  as for moeq_attn_paged; positions in no page of the cache are left out
  * No two requests' tables may share the pages behind their contexts.
  * Errors: INVALID_ARG, UNSUPPORTED, DEVICE. */
@@ -688,6 +689,15 @@ moeq_status moeq_kv_commit(const moeq_kv_cache* cache, const moeq_kv_scales* sca
                            int32_t max_path, const int32_t* counts, const int32_t* ctx_lens,
                            const int32_t* block_table, int64_t table_stride, int32_t max_blocks, int32_t n_requests,
                            void* stream);
+/* The same where only the positions below kv_lens[r] are the request's: what lies behind
+ * them is neither read nor moved, whatever counts says.  With moeq_kv_plan's kv_lens a
+ * refused request (0) keeps all of the cache as it is.
+ *   kv_lens  DEVICE int32 [n_requests] */
+moeq_status moeq_kv_commit_within(const moeq_kv_cache* cache, const moeq_kv_scales* scales, int32_t n_kv_heads,
+                                  int32_t head_dim, int32_t value_dim, const int32_t* path, int64_t path_stride,
+                                  int32_t max_path, const int32_t* counts, const int32_t* ctx_lens,
+                                  const int32_t* kv_lens, const int32_t* block_table, int64_t table_stride,
+                                  int32_t max_blocks, int32_t n_requests, void* stream);
 
 /* Gives the pages that requests no longer need back to the ring of free pages: of
  * request r's pages for kv_lens[r] tokens, those beyond the ones for its first

@@ -104,12 +104,15 @@ def append(k_cache, v_cache, k, v, slots, *, scales=None, stream=None):
     _c.append(k_cache, v_cache, k, v, slots, scales, stream)
 
 
-def commit(k_cache, v_cache, path, counts, ctx_lens, block_table, *, scales=None, stream=None):
+def commit(k_cache, v_cache, path, counts, ctx_lens, block_table, *, kv_lens=None, scales=None, stream=None):
     """Keeps the drafted tokens path[r, :counts[r]] (int32 [R, any], numbers among the
     request's new tokens, ascending from 0) in the cache: their keys and values move to
-    the places right behind the ctx_lens[r] tokens before them.  A request that the
-    step's plan refused (kv_lens[r] is 0) needs a count of 0."""
-    _c.commit(k_cache, v_cache, path, counts, ctx_lens, block_table, scales, stream)
+    the places right behind the ctx_lens[r] tokens before them.
+    kv_lens: the step plan's (int32 [R]); what lies behind a request's kv_lens[r] tokens
+    is not its own and stays, so that a request that the plan refused (0) moves nothing.
+    Without it such a request needs a count of 0 or 1 (drafts.verify counts its tokens
+    as any others')."""
+    _c.commit(k_cache, v_cache, path, counts, ctx_lens, block_table, scales, kv_lens, stream)
 
 
 def trim(kv_lens, kept_lens, block_table, free_pages, pool, *, page_size, pool_out=None, stream=None):

@@ -352,7 +352,7 @@ PyObject* paged_workspace(PyObject* const* a) {
   return PyLong_FromUnsignedLongLong(bytes);
 }
 
-// k_cache, v_cache, path, counts, ctx_lens, block_table, scales, stream
+// k_cache, v_cache, path, counts, ctx_lens, block_table, scales, kv_lens, stream
 PyObject* commit(PyObject* const* a) {
   const at::Tensor& k = first(a[0], "k_cache");
   if (a[6] == Py_None) dtype_code(k.scalar_type());
@@ -362,12 +362,17 @@ PyObject* commit(PyObject* const* a) {
   const int64_t R = path.size(0), width = path.size(1);
   const int32_t *cp = ints(a[3], "counts", R, k), *xp = ints(a[4], "ctx_lens", R, k);
   const at::Tensor& table = check(a[5], "block_table", at::kInt, Shape{{R, kAny}, 2}, k);
-  const int64_t blocks = table.size(1);
-  done(moeq_kv_commit(&c.c, sc.get(), narrow(c.heads, "the number of kv heads"), narrow(c.dim, "the head dimension"),
-                      narrow(c.value_dim, "the value dimension"), (const int32_t*)path.data_ptr(),
-                      R > 1 ? path.stride(0) : width, narrow(width, "the paths' width"), cp, xp,
-                      (const int32_t*)table.data_ptr(), R > 1 ? table.stride(0) : blocks,
-                      narrow(blocks, "the table's width"), narrow(R, "the number of requests"), stream(a[7], k)));
+  const int32_t heads = narrow(c.heads, "the number of kv heads"), dim = narrow(c.dim, "the head dimension"),
+                value_dim = narrow(c.value_dim, "the value dimension"), w = narrow(width, "the paths' width"),
+                blocks = narrow(table.size(1), "the table's width"), r = narrow(R, "the number of requests");
+  const int64_t path_row = R > 1 ? path.stride(0) : width, pitch = R > 1 ? table.stride(0) : blocks;
+  const int32_t *pp = (const int32_t*)path.data_ptr(), *tp = (const int32_t*)table.data_ptr();
+  if (a[7] == Py_None)
+    done(moeq_kv_commit(&c.c, sc.get(), heads, dim, value_dim, pp, path_row, w, cp, xp, tp, pitch, blocks, r,
+                        stream(a[8], k)));
+  else
+    done(moeq_kv_commit_within(&c.c, sc.get(), heads, dim, value_dim, pp, path_row, w, cp, xp, ints(a[7], "kv_lens", R, k),
+                               tp, pitch, blocks, r, stream(a[8], k)));
   cache_written(a[0], a[1], a[6]);
   Py_RETURN_NONE;
 }
@@ -487,7 +492,7 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define MOEQ_METHOD(f, n) \
   { #f, (PyCFunction)(void (*)(void))call<f, n>, METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {MOEQ_METHOD(plan, 10),   MOEQ_METHOD(append, 7),           MOEQ_METHOD(prompt, 10),
-                         MOEQ_METHOD(paged, 16),  MOEQ_METHOD(paged_workspace, 5),  MOEQ_METHOD(commit, 8),
+                         MOEQ_METHOD(paged, 16),  MOEQ_METHOD(paged_workspace, 5),  MOEQ_METHOD(commit, 9),
                          MOEQ_METHOD(trim, 8),    MOEQ_METHOD(verify, 11),          MOEQ_METHOD(verify_workspace, 2),
                          MOEQ_METHOD(setup, 3),   {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_attention", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -109,7 +109,7 @@ struct CommitArgs {
   int64_t k_page, k_row, k_head, v_page, v_row, v_head;  // bytes
   uint8_t *ks, *vs;                                      // or null
   int64_t ks_page, ks_head, vs_page, vs_head;
-  const int32_t *path, *counts, *ctx, *table;
+  const int32_t *path, *counts, *ctx, *kv, *table;       // kv may be null
   int64_t table_stride, path_stride;
   int32_t R, width, HK, kchunks, vchunks, n_pages, page_shift, max_blocks;
 };

@@ -306,6 +306,74 @@ moeq_status attn_over_cache(const moeq_attn* a, const moeq_rows* q, const moeq_k
               "paged attention launch");
 }
 
+// kv_lens may be null
+moeq_status commit(const moeq_kv_cache* cache, const moeq_kv_scales* scales, int32_t n_kv_heads, int32_t head_dim,
+                   int32_t value_dim, const int32_t* path, int64_t path_stride, int32_t max_path, const int32_t* counts,
+                   const int32_t* ctx_lens, const int32_t* kv_lens, const int32_t* block_table, int64_t table_stride,
+                   int32_t max_blocks, int32_t n_requests, void* stream) {
+  const int size = scales ? 1 : 2;
+  if (n_kv_heads < 1 || n_kv_heads > kMaxHeads)
+    return fail(MOEQ_ERR_INVALID_ARG, "n_kv_heads %d must lie in 1 .. %d", n_kv_heads, kMaxHeads);
+  moeq_status st;
+  if (scales) {
+    if ((st = check_codes(head_dim, value_dim)) != MOEQ_OK) return st;
+  } else if (head_dim < 8 || value_dim < 8 || head_dim % 8 || value_dim % 8 || head_dim > 1024 || value_dim > 1024) {
+    return fail(MOEQ_ERR_INVALID_ARG, "head_dim %d and value_dim %d must be multiples of 8 up to 1024", head_dim,
+                value_dim);
+  }
+  if ((st = check_cache(cache, scales != nullptr)) != MOEQ_OK ||
+      (st = check_apart(cache, n_kv_heads, head_dim, value_dim)) != MOEQ_OK)
+    return st;
+  if (scales &&
+      ((st = check_scales(scales)) != MOEQ_OK || (st = check_scales_apart(scales, cache, n_kv_heads)) != MOEQ_OK))
+    return st;
+  if (max_blocks < 1 || table_stride < max_blocks)
+    return fail(MOEQ_ERR_INVALID_ARG, "max_blocks %d must be positive and at most table_stride", max_blocks);
+  if (n_requests < 0 || n_requests > kMaxRows || max_path < 0 || max_path > kMaxRows || path_stride < max_path)
+    return fail(MOEQ_ERR_INVALID_ARG, "n_requests %d and max_path %d must lie in 0 .. 2^24, max_path within path_stride",
+                n_requests, max_path);
+  if (n_requests == 0 || max_path == 0) return MOEQ_OK;
+  if (!path || !counts || !ctx_lens || !block_table || !aligned4(path) || !aligned4(counts) || !aligned4(ctx_lens) ||
+      !aligned4(block_table))
+    return fail(MOEQ_ERR_INVALID_ARG, "path, counts, ctx_lens and block_table must be 4-byte aligned and not NULL");
+  CommitArgs g{};
+  g.k = (char*)cache->k;
+  g.v = (char*)cache->v;
+  g.k_page = cache->k_page_stride * size;
+  g.k_row = cache->k_slot_stride * size;
+  g.k_head = cache->k_head_stride * size;
+  g.v_page = cache->v_page_stride * size;
+  g.v_row = cache->v_slot_stride * size;
+  g.v_head = cache->v_head_stride * size;
+  if (scales) {
+    g.ks = (uint8_t*)scales->k;
+    g.vs = (uint8_t*)scales->v;
+    g.ks_page = scales->k_page_stride;
+    g.ks_head = scales->k_head_stride;
+    g.vs_page = scales->v_page_stride;
+    g.vs_head = scales->v_head_stride;
+  }
+  g.path = path;
+  g.counts = counts;
+  g.ctx = ctx_lens;
+  g.kv = kv_lens;
+  g.table = block_table;
+  g.table_stride = table_stride;
+  g.path_stride = path_stride;
+  g.R = n_requests;
+  g.width = max_path;
+  g.HK = n_kv_heads;
+  g.kchunks = head_dim * size / 16;
+  g.vchunks = value_dim * size / 16;
+  g.n_pages = cache->n_pages;
+  g.page_shift = log2_of(cache->page_size);
+  g.max_blocks = max_blocks;
+  const int64_t lanes = (int64_t)n_kv_heads * (std::max(g.kchunks, g.vchunks) + 1);
+  if ((lanes + 255) / 256 * n_requests > kMaxThreads / 256)
+    return fail(MOEQ_ERR_UNSUPPORTED, "%d requests of %d kv heads exceed a launch", n_requests, n_kv_heads);
+  return done(launch_kv_commit(g, (hipStream_t)stream), "commit launch");
+}
+
 }  // namespace
 
 extern "C" {
@@ -469,66 +537,19 @@ moeq_status moeq_kv_commit(const moeq_kv_cache* cache, const moeq_kv_scales* sca
                            int32_t max_path, const int32_t* counts, const int32_t* ctx_lens,
                            const int32_t* block_table, int64_t table_stride, int32_t max_blocks, int32_t n_requests,
                            void* stream) {
-  const int size = scales ? 1 : 2;
-  if (n_kv_heads < 1 || n_kv_heads > kMaxHeads)
-    return fail(MOEQ_ERR_INVALID_ARG, "n_kv_heads %d must lie in 1 .. %d", n_kv_heads, kMaxHeads);
-  moeq_status st;
-  if (scales) {
-    if ((st = check_codes(head_dim, value_dim)) != MOEQ_OK) return st;
-  } else if (head_dim < 8 || value_dim < 8 || head_dim % 8 || value_dim % 8 || head_dim > 1024 || value_dim > 1024) {
-    return fail(MOEQ_ERR_INVALID_ARG, "head_dim %d and value_dim %d must be multiples of 8 up to 1024", head_dim,
-                value_dim);
-  }
-  if ((st = check_cache(cache, scales != nullptr)) != MOEQ_OK ||
-      (st = check_apart(cache, n_kv_heads, head_dim, value_dim)) != MOEQ_OK)
-    return st;
-  if (scales &&
-      ((st = check_scales(scales)) != MOEQ_OK || (st = check_scales_apart(scales, cache, n_kv_heads)) != MOEQ_OK))
-    return st;
-  if (max_blocks < 1 || table_stride < max_blocks)
-    return fail(MOEQ_ERR_INVALID_ARG, "max_blocks %d must be positive and at most table_stride", max_blocks);
-  if (n_requests < 0 || n_requests > kMaxRows || max_path < 0 || max_path > kMaxRows || path_stride < max_path)
-    return fail(MOEQ_ERR_INVALID_ARG, "n_requests %d and max_path %d must lie in 0 .. 2^24, max_path within path_stride",
-                n_requests, max_path);
-  if (n_requests == 0 || max_path == 0) return MOEQ_OK;
-  if (!path || !counts || !ctx_lens || !block_table || !aligned4(path) || !aligned4(counts) || !aligned4(ctx_lens) ||
-      !aligned4(block_table))
-    return fail(MOEQ_ERR_INVALID_ARG, "path, counts, ctx_lens and block_table must be 4-byte aligned and not NULL");
-  CommitArgs g{};
-  g.k = (char*)cache->k;
-  g.v = (char*)cache->v;
-  g.k_page = cache->k_page_stride * size;
-  g.k_row = cache->k_slot_stride * size;
-  g.k_head = cache->k_head_stride * size;
-  g.v_page = cache->v_page_stride * size;
-  g.v_row = cache->v_slot_stride * size;
-  g.v_head = cache->v_head_stride * size;
-  if (scales) {
-    g.ks = (uint8_t*)scales->k;
-    g.vs = (uint8_t*)scales->v;
-    g.ks_page = scales->k_page_stride;
-    g.ks_head = scales->k_head_stride;
-    g.vs_page = scales->v_page_stride;
-    g.vs_head = scales->v_head_stride;
-  }
-  g.path = path;
-  g.counts = counts;
-  g.ctx = ctx_lens;
-  g.table = block_table;
-  g.table_stride = table_stride;
-  g.path_stride = path_stride;
-  g.R = n_requests;
-  g.width = max_path;
-  g.HK = n_kv_heads;
-  g.kchunks = head_dim * size / 16;
-  g.vchunks = value_dim * size / 16;
-  g.n_pages = cache->n_pages;
-  g.page_shift = log2_of(cache->page_size);
-  g.max_blocks = max_blocks;
-  const int64_t lanes = (int64_t)n_kv_heads * (std::max(g.kchunks, g.vchunks) + 1);
-  if ((lanes + 255) / 256 * n_requests > kMaxThreads / 256)
-    return fail(MOEQ_ERR_UNSUPPORTED, "%d requests of %d kv heads exceed a launch", n_requests, n_kv_heads);
-  return done(launch_kv_commit(g, (hipStream_t)stream), "commit launch");
+  return commit(cache, scales, n_kv_heads, head_dim, value_dim, path, path_stride, max_path, counts, ctx_lens, nullptr,
+                block_table, table_stride, max_blocks, n_requests, stream);
+}
+
+moeq_status moeq_kv_commit_within(const moeq_kv_cache* cache, const moeq_kv_scales* scales, int32_t n_kv_heads,
+                                  int32_t head_dim, int32_t value_dim, const int32_t* path, int64_t path_stride,
+                                  int32_t max_path, const int32_t* counts, const int32_t* ctx_lens,
+                                  const int32_t* kv_lens, const int32_t* block_table, int64_t table_stride,
+                                  int32_t max_blocks, int32_t n_requests, void* stream) {
+  if (n_requests > 0 && max_path > 0 && (!kv_lens || !aligned4(kv_lens)))
+    return fail(MOEQ_ERR_INVALID_ARG, "kv_lens must be 4-byte aligned and not NULL");
+  return commit(cache, scales, n_kv_heads, head_dim, value_dim, path, path_stride, max_path, counts, ctx_lens, kv_lens,
+                block_table, table_stride, max_blocks, n_requests, stream);
 }
 
 moeq_status moeq_kv_trim(const int32_t* kv_lens, const int32_t* kept_lens, int32_t n_requests,

@@ -146,6 +146,7 @@ def _load():
         "moeq_verify": [P, P, P, I32, I32, I32, I32, P, I64, P, I64, P, P, P, P, P, P, U64, P],
         "moeq_verify_workspace": [I32, I32, ctypes.POINTER(U64)],
         "moeq_kv_commit": [CACHE, SCALES, I32, I32, I32, P, I64, I32, P, P, P, I64, I32, I32, P],
+        "moeq_kv_commit_within": [CACHE, SCALES, I32, I32, I32, P, I64, I32, P, P, P, P, I64, I32, I32, P],
         "moeq_kv_trim": [P, P, I32, P, I64, I32, P, I32, P, P, I32, P],
     }
     for name, args in sig.items():
@@ -367,6 +368,13 @@ def moeq_kv_commit(cache, scales, n_kv_heads, head_dim, value_dim, path, path_st
     """cache: moeq_kv_cache; scales: moeq_kv_scales or None; the arrays device addresses."""
     _check(lib.moeq_kv_commit(cache, scales, n_kv_heads, head_dim, value_dim, path, path_stride, max_path, counts, ctx_lens,
                               block_table, table_stride, max_blocks, n_requests, stream or None))
+
+
+def moeq_kv_commit_within(cache, scales, n_kv_heads, head_dim, value_dim, path, path_stride, max_path, counts, ctx_lens, kv_lens,
+                          block_table, table_stride, max_blocks, n_requests, stream=0):
+    """As moeq_kv_commit; kv_lens: device address."""
+    _check(lib.moeq_kv_commit_within(cache, scales, n_kv_heads, head_dim, value_dim, path, path_stride, max_path, counts, ctx_lens,
+                                     kv_lens, block_table, table_stride, max_blocks, n_requests, stream or None))
 
 
 def moeq_kv_trim(kv_lens, kept_lens, n_requests, block_table, table_stride, max_blocks, free_pages, n_pages, pool_in, pool_out,
