@@ -652,7 +652,7 @@ moeq_status moeq_attn_tree(const moeq_attn* a, const moeq_rows* q, const moeq_kv
  *   max_new   0 .. 256: at least the most tokens of a request (a larger one is left out)
  *   vocab     1 .. 2^20
  *   target, draft  DEVICE float [n_tokens x vocab], rows target_stride (draft_stride) >=
- *             vocab apart; draft may be NULL
+ *             vocab apart; draft may be NULL (with it fewer than 2^22 requests)
  *   uniform   DEVICE float [n_tokens], in [0, 1) (the roots' are not used)
  *   last      DEVICE float [n_requests], in [0, 1)
  *   path      DEVICE int32 [n_requests x max_new] (written): the numbers of the root and

@@ -150,6 +150,7 @@ struct VerifyArgs {
   double* sums;  // [R x n_chunks]
 };
 constexpr int kMaxVocab = 1 << 20;
+constexpr int kWalkThreads = 1024;  // a request's, where its walk has a launch of its own
 int verify_chunks(int V);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
 

@@ -593,6 +593,8 @@ moeq_status moeq_verify(const int32_t* tokens, const int32_t* parents, const int
     return fail(max_new < 0 ? MOEQ_ERR_INVALID_ARG : MOEQ_ERR_UNSUPPORTED, "max_new %d must lie in 0 .. %d", max_new,
                 kMaxTree);
   if (n_requests == 0) return MOEQ_OK;
+  if (draft && (int64_t)n_requests * kWalkThreads > kMaxThreads)
+    return fail(MOEQ_ERR_UNSUPPORTED, "%d requests with draft rows exceed a launch", n_requests);
   if (n_tokens > 1 && (target_stride < vocab || (draft && draft_stride < vocab) || target_stride >= (int64_t)1 << 40 ||
                        draft_stride >= (int64_t)1 << 40))
     return fail(MOEQ_ERR_INVALID_ARG, "rows of %d probabilities overlap at strides of %lld and %lld", vocab,

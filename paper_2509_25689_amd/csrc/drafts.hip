@@ -215,7 +215,6 @@ __device__ __forceinline__ Walk walk(const VerifyArgs& a, int r, bool write, Wal
 // 128000 (1 MB) takes 15 us, with 256 threads 35 (reads of a step ahead do not gain: a
 // third of it is float64 arithmetic); 48 chains, which need none, 6 us in all (8 with every
 // wave on the way of the first).
-constexpr int kWalkThreads = 1024;
 __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyArgs a) {
   __shared__ WalkShared<kWalkThreads> sh;
   walk(a, blockIdx.x, true, sh);
