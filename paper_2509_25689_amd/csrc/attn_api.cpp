@@ -595,8 +595,8 @@ moeq_status moeq_verify(const int32_t* tokens, const int32_t* parents, const int
   if (n_requests == 0) return MOEQ_OK;
   if (draft && (int64_t)n_requests * kWalkThreads > kMaxThreads)
     return fail(MOEQ_ERR_UNSUPPORTED, "%d requests with draft rows exceed a launch", n_requests);
-  if (n_tokens > 1 && (target_stride < vocab || (draft && draft_stride < vocab) || target_stride >= (int64_t)1 << 40 ||
-                       draft_stride >= (int64_t)1 << 40))
+  const auto row_ok = [&](int64_t stride) { return stride >= vocab && stride < (int64_t)1 << 40; };
+  if (n_tokens > 1 && (!row_ok(target_stride) || (draft && !row_ok(draft_stride))))
     return fail(MOEQ_ERR_INVALID_ARG, "rows of %d probabilities overlap at strides of %lld and %lld", vocab,
                 (long long)target_stride, (long long)draft_stride);
   if (!cu || !counts || !last) return fail(MOEQ_ERR_INVALID_ARG, "cu, counts and last must not be NULL");

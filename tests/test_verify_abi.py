@@ -19,3 +19,10 @@ def _call(**kw):
 def test_requests_of_a_walk_beyond_a_launch(R):
     """With draft rows a request's walk has 1024 threads: 2^22 requests are 2^32, more than a launch has."""
     assert _call(R=R) == UNSUP and "exceed a launch" in moeq.moeq_last_error()
+
+
+@pytest.mark.parametrize("stride", [0, -5, 1 << 40, (1 << 63) - 1])
+def test_stride_without_draft_rows(stride):
+    """Without draft rows their stride says nothing: the call comes as far as its workspace's size."""
+    assert _call(draft=None, dstride=stride, size=0) == CAP
+    assert _call(dstride=stride, size=0) == BAD
