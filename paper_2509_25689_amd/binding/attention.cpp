@@ -419,6 +419,9 @@ PyObject* verify(PyObject* const* a) {
   const int64_t W = number(a[7]);
   if (W < 0) throw Raise{PyExc_ValueError, "max_new must not be negative"};
   const int32_t r = narrow(R, "the number of requests"), v = narrow(V, "the vocabulary"), w = narrow(W, "max_new");
+  // what there is to refuse in the sizes, before memory is taken for them (no requests: nothing is done)
+  done(moeq_verify(nullptr, nullptr, nullptr, 0, 0, w, v, nullptr, 0, nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr,
+                   nullptr, 0, nullptr));
   uint64_t bytes = 0;
   at::Tensor ws;
   if (a[9] == Py_None) {

@@ -27,7 +27,7 @@ def verify(tokens, parents, cu, target, draft, uniform, last, *, max_new, worksp
     tokens [R, max_new] (the kept tokens after the root and the one that follows, then -1).
     """
     buffer = None
-    if stream is not None and attention._is(target, 2) and attention._is(cu, 1) and cu.numel() and max_new >= 0:
+    if stream is not None and attention._is(target, 2) and attention._is(cu, 1) and cu.numel() and 0 <= max_new <= 256:
         R = cu.numel() - 1
         buffer = attention._new(target, R * (2 * max_new + 1), torch.int32, stream)
         if workspace is None:
