@@ -75,9 +75,9 @@ def main(shape="tree", cache="bf16", requests=5, n_tokens=40, depth=4, width=3, 
     places, page_size = 3, 16
     lengths = [3 + 17 * i % 60 for i in range(requests)]
     most = 1 + depth * width
-    blocks = -(-(max(lengths) + n_tokens + 2 * most) // page_size) + 1
+    blocks = -(-(max(lengths, default=0) + n_tokens + 2 * most) // page_size) + 1
     n_pages = places * blocks
-    model = Model(vocab, max_tokens=1024)
+    model = Model(vocab, max_tokens=max(1024, blocks * page_size))  # (the last pass takes a request's tokens as one prompt)
     block = model.block
     codes = cache == "e4m3"
     k_cache, v_cache = attention.empty_cache(n_pages, page_size, block.kv_heads, block.dim,
@@ -176,10 +176,11 @@ def main(shape="tree", cache="bf16", requests=5, n_tokens=40, depth=4, width=3, 
         worst = max(worst, float((got - want).norm() / want.norm()))
     back = int(pool[1]) == n_pages and sorted(free.tolist()) == list(range(n_pages))
     block.layer.close()
+    per_step = given / max(steps, 1)
     if verbose:
-        print(f"{requests} requests, {given} tokens in {steps} steps of a request ({given / steps:.2f} each); outputs differ from whole "
+        print(f"{requests} requests, {given} tokens in {steps} steps of a request ({per_step:.2f} each); outputs differ from whole "
               f"prompts' by {worst:.2e}; every page back: {back}")
-    return worst, given / steps, back
+    return worst, per_step, back
 
 
 if __name__ == "__main__":
