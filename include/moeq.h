@@ -602,7 +602,10 @@ moeq_status moeq_kv_append_e4m3(const moeq_attn* a, const moeq_kv_cache* cache, 
 
 /* moeq_attn_paged over such a cache.  a's dtype is that of q and out; the products take
  * codes and scales as the values they stand for, in dtype's range (a MOEQ_F16 cache is
- * one that was written as such).  The scales' bytes lie in 1 .. 254.  Workspace and
+ * one that was written as such).  The scales' bytes lie in 1 .. 254.  A weight times its
+ * value's scale may be held as a bfloat16, whose steps are 2^-133 at least: of MOEQ_BF16
+ * rows whose values lie below about 2^-110 (scales 2^-118) small weights keep fewer bits,
+ * 2^-134 / scale of the largest weight being the most that one is off.  Workspace and
  * errors as for moeq_attn_paged. */
 moeq_status moeq_attn_paged_e4m3(const moeq_attn* a, const moeq_rows* q, const moeq_kv_cache* cache,
                                  const moeq_kv_scales* scales, const int32_t* cu_q, const int32_t* kv_lens,

@@ -60,7 +60,9 @@ __device__ __forceinline__ void load_lds4(const char* from, uint32_t dst) {
 __device__ __forceinline__ uint32_t lds_read4(uint32_t a) { return *(const MOEQ_LDS uint32_t*)(uintptr_t)a; }
 
 // Weights times their values' scales (byte j of v for the j-th), rounded, as the second
-// operand of the product with the values: a dword holds two.
+// operand of the product with the values: a dword holds two.  (Below 2^-126 a bfloat16 is
+// off by up to 2^-134 whatever it is: that is all that a weight loses, and it takes scales
+// below 2^-118 to be more than 2^-16 of the largest.  A lift would need room above 2^127.)
 template <int TERMS>
 __device__ __forceinline__ void scaled_pair(float w0, float w1, uint32_t v, int j, uint32_t (&p)[TERMS]) {
   // (0 times whatever the scale of a key that does not exist is 0)
