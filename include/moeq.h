@@ -642,7 +642,11 @@ moeq_status moeq_attn_tree(const moeq_attn* a, const moeq_rows* q, const moeq_kv
  * (taken to sum to z = 1):
  *   with draft (row t: the distribution that t's children were drawn from), child c of
  *   token x is kept if uniform[c] draft[t][x] z < r[x]; a rejected one leaves
- *   max(r - z draft[t], 0), and z its sum;
+ *   max(r - z draft[t], 0), and z its sum.  (Several children of a token have to be drawn
+ *   independently, each from the whole row, twins allowed: of children drawn without
+ *   replacement the result is not distributed as the target.  Each child after a rejected
+ *   one takes a pass over both rows that repeats the rejections before it, so the time
+ *   grows with the square of a token's rejected children: meant for a few of them);
  *   with draft NULL (drafts that were not drawn: the likeliest tokens, a lookup's), it
  *   is kept if uniform[c] z < r[x]; a rejected one leaves r with r[x] = 0, and z - r[x].
  * Where no child is kept, the next token is the first j with r[0] + .. + r[j] > last[r] *

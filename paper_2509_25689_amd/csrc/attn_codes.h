@@ -362,8 +362,9 @@ struct Codes16 {
 
 // ---- the kernel ----
 // A stage holds 32 keys, their values and, in its last 256 bytes, both scales (64 bytes;
-// the load fills the rest with the same).  128 KB of LDS or more are in flight:
-// eight waves of two stages with 128-wide heads.
+// the load fills the rest with the same).  Loads of 132 KB of LDS are in flight with
+// 128-wide heads (eight waves of two stages), 136 with 64-wide ones (eight of four), 123
+// with 192-wide ones (six of two).
 constexpr int few8_waves(int D) { return D == 192 ? 6 : 8; }
 template <int D, int DV, int ROWS>
 struct FewKernel8 {

@@ -391,8 +391,8 @@ struct RowBlock {
   // where o is not finite after them it is formed anew, key by key on the vector
   // units, from the keys each row sees among the `width` keys of each of `tiles`
   // tiles, tile_key(i) the first; a row sees a key of [lo, hi) if sees(key).  Keys from
-  // `end` on do not exist.  keys.chunk(key, c) are 8 values of a key, keys.four(key, c)
-  // 4 of its value (from memory).  m and l hold already.
+  // `end` on do not exist.  keys.key_row(key).chunk(c) are 8 values of a key,
+  // keys.value_row(key).four(c) 4 of its value (from memory).  m and l hold already.
   __device__ __forceinline__ bool finite() const {
     // (largest magnitude; a NaN makes the sum NaN)
     float t = 0.0f;

@@ -29,9 +29,13 @@ hipError_t launch_paged(AttnArgs a, int dtype, int D, int64_t max_rows, char* ws
     a.whole = a.max_kv <= 512;
     // Which requests the few-rows kernel takes: those of up to 32 rows.  Over codes those
     // of up to 16 where no other is there, or where the others go to tiles: 48 requests
-    // of 7 rows take 62 us a call so and 65 in blocks of 32.  A step of trees larger than
-    // that is left to the tiles whole: a small tree among them costs less there than two
-    // more launches.
+    // of 7 rows take 62 us a call so and 65 in blocks of 32.  A step of trees whose
+    // max_rows is larger than that is left to the tiles whole: a few small trees among
+    // large ones cost less there than two more launches.  The price is a step of small
+    // trees with one large one, or with a max_new above what it holds: 48 requests of one
+    // token of 7 heads over 400 MB of codes 76 us a call with max_new 1 and 135 with 16
+    // (4 tokens: 89 with 4, 139 with 16; one tree of 16 among single tokens 136; all of 16
+    // 163), over 16-bit values 119 and 161 (129 and 161; 161; 172).
     a.few_rows = TREE && tiles ? 0 : E4M3 && a.g <= 16 && (tiles || max_rows <= 16) ? 16 : kFewRows;
     hipError_t e = hipSuccess;
     if (a.few_rows == 0) {

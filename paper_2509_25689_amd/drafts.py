@@ -19,12 +19,16 @@ def verify(tokens, parents, cu, target, draft, uniform, last, *, max_new, worksp
     tokens, parents  int32 [T]; cu int32 [R + 1]: the requests' trees, roots first
     target   float32 [T, V]: the target's distribution after each token
     draft    float32 [T, V]: the distribution that each token's children were drawn
-             from, or None for drafts that were not drawn
+             from, independently of each other (not without replacement: the result
+             would not be distributed as the target), or None for drafts that were
+             not drawn, as the likeliest tokens are not
     uniform  float32 [T], last float32 [R]: random numbers in [0, 1)
     max_new  at least the most tokens of a request, at most 256
     workspace  a uint8 tensor of verify_workspace(R, V) bytes, else made here
     -> path [R, max_new] (numbers of the root and the kept tokens, then -1), counts [R],
     tokens [R, max_new] (the kept tokens after the root and the one that follows, then -1).
+    A request that the step's plan refused is walked as any other: where kv_lens is 0 its
+    counts and tokens mean nothing (attention.commit takes kv_lens and leaves it alone).
     """
     buffer = None
     if stream is not None and attention._is(target, 2) and attention._is(cu, 1) and cu.numel() and 0 <= max_new <= 256:
